@@ -511,6 +511,148 @@ RTCC_API rtcc_status rtcc_rotated_nms_noalloc(const float *device_records, int64
                                               void *hip_stream);
 
 /* ------------------------------------------------------------------------
+ * Token operators: what a model does with tokens of the fused map (patches of
+ * cells, frame after frame) after the join.  Context-free; on the current HIP
+ * device; every call enqueues on hip_stream (NULL = the null stream), returns
+ * without waiting and may be captured into a HIP graph.  Tensors are device
+ * memory of the caller's and must stay valid until the stream has passed the
+ * call.  Element types follow `precision` (rtcc_precision: float32 or
+ * bfloat16); all sums, norms and softmax statistics are float32, and a bf16
+ * result is rounded once (RNE).  A row is one token.  Tensors are [rows][heads]
+ * [head_dim] with element strides stride[0] (row) and stride[1] (head); the
+ * channels of a head are contiguous.  Pointers and strides keep every head
+ * 16-byte aligned; strides are at least head_dim, between rows at most 2^22
+ * and between heads at most 2^40 elements (a stride of an axis with one entry
+ * is not looked at).  head_dim is a multiple of 16, at most 128.  Outputs must not overlap inputs unless said
+ * otherwise.  Errors: RTCC_E_ARG for anything a check below names, RTCC_E_HIP
+ * for a failed launch; the message is rtcc_last_error(NULL).  Every check is
+ * made before the first launch: a call that is refused has written nothing.
+ * ------------------------------------------------------------------------ */
+
+#define RTCC_MAX_AXES 3
+
+/* Norm and rotation of queries and keys, in one pass (rtcc_norm_rope).  For
+ * every row and head of x = q, k:
+ *   n = x / sqrt(mean(x^2) + eps) * w          (w: the head's norm weight)
+ *   pair p of n (channels 2p, 2p + 1 with interleaved = 1; else p and
+ *   p + head_dim / 2) is rotated by the angle
+ *   positions[row][a] * inv_freq[p], a = the axis whose section holds p
+ * sections[a] pairs follow each other axis by axis (time, row, column, as the
+ * caller orders them); pairs past the last section are not rotated.  Angles
+ * are reduced in float64.
+ * Appending to a cache: with slots (device int64 [rows]) row r of k goes to
+ * row slots[r] of k_out, of slot_rows rows, and row r of v, if given, is
+ * copied to the same row of v_out; a slot outside [0, slot_rows) is skipped.
+ * Two rows with one slot: either may be kept.  Without slots row r goes to
+ * row r.  q_out may be q, and k_out k without slots, with the same strides. */
+typedef struct rtcc_norm_rope_desc {
+    int32_t abi_version;          /* RTCC_ABI_VERSION                                   */
+    int32_t precision;            /* rtcc_precision of q, k, v and the outputs          */
+    int64_t rows;                 /* tokens, 0 .. 2^31 - 1                              */
+    int64_t slot_rows;            /* rows of k_out and v_out with slots; else unused    */
+    int32_t q_heads, kv_heads;    /* 0 .. 1024, not both 0; a tensor without heads may be NULL */
+    int32_t head_dim;
+    int32_t interleaved;          /* 0 or 1                                             */
+    int32_t n_axes;               /* 1 .. RTCC_MAX_AXES                                 */
+    int32_t sections[RTCC_MAX_AXES]; /* pairs of each axis, >= 0, at most head_dim / 2 in all */
+    float eps;                    /* finite, >= 0                                       */
+    const void *q, *k, *v;        /* v: NULL without slots; optional with them          */
+    void *q_out, *k_out, *v_out;
+    int64_t q_stride[2], k_stride[2], v_stride[2];
+    int64_t q_out_stride[2], k_out_stride[2], v_out_stride[2];
+    const float *q_weight, *k_weight; /* [head_dim], or [heads][head_dim]; NULL: all 1  */
+    int32_t q_weight_per_head, k_weight_per_head; /* 0: one weight for all heads        */
+    const float *positions;       /* [rows][n_axes], contiguous                         */
+    const float *inv_freq;        /* [sum of sections]                                  */
+    const int64_t *slots;         /* [rows] or NULL                                     */
+} rtcc_norm_rope_desc;
+RTCC_API rtcc_status rtcc_norm_rope(const rtcc_norm_rope_desc *desc, void *hip_stream);
+
+/* Gradients of rtcc_norm_rope.  fwd describes the forward call; of its tensors
+ * only q, k, the weights, positions and inv_freq are read (q_out, k_out, v,
+ * v_out and slots are ignored).  dq_out, dk_out: the gradients of the outputs,
+ * row r at row r.  dq, dk: as q, k; dq may be dq_out and dk dk_out, with the
+ * same strides.  dq_weight, dk_weight: float32, of the weights' shape ([head_dim]
+ * where fwd has none), written, not added to; summed over rows (and heads) in
+ * a fixed order; NULL: not wanted.  workspace: device memory of at least
+ * rtcc_norm_rope_grad_workspace bytes, 16-byte aligned (NULL where that is 0). */
+typedef struct rtcc_norm_rope_grad_desc {
+    rtcc_norm_rope_desc fwd;
+    const void *dq_out, *dk_out;
+    void *dq, *dk;
+    int64_t dq_out_stride[2], dk_out_stride[2], dq_stride[2], dk_stride[2];
+    float *dq_weight, *dk_weight;
+} rtcc_norm_rope_grad_desc;
+RTCC_API rtcc_status rtcc_norm_rope_grad_workspace(const rtcc_norm_rope_grad_desc *desc, size_t *bytes);
+RTCC_API rtcc_status rtcc_norm_rope_grad(const rtcc_norm_rope_grad_desc *desc, void *workspace, size_t workspace_bytes,
+                                         void *hip_stream);
+
+/* Attention of packed sequences (rtcc_attention).  Sequence s has the queries
+ * [q_offsets[s], q_offsets[s + 1]) of q's rows and the keys [k_offsets[s],
+ * k_offsets[s] + k_lens[s]) of k's and v's rows (k_lens NULL: k_offsets has
+ * n_seqs + 1 entries and sequence s ends where s + 1 begins): scenes packed
+ * into one batch, or caches of one capacity each.  A token sees tokens of its
+ * own sequence only.  With nq queries and nk keys query i stands at key place
+ * p = nk - nq + i (the newest tokens last), and sees key j iff
+ *   causal = 0:  j < nk
+ *   causal = 1:  j < nk and (j <= p or j < prefix_lens[s])
+ * Query head h reads key head h / (q_heads / kv_heads).  For visible pairs
+ *   x = scale * <q, k>;  with softcap > 0: x = softcap * tanh(x / softcap);
+ *   with slopes: x -= slopes[h] * |p - j|
+ *   out = sum_j softmax_j(x) v_j,   lse = log sum_j exp(x)
+ * A query that sees no key (or only scores of -inf) has out = 0, lse = -inf.
+ * Keys that a query does not see take no part, whatever they hold.  Rows of q
+ * in no sequence are not written.  Every offset and length is clamped to the
+ * buffers (q_rows, k_rows) and to sequences in ascending order, so that no
+ * list, whatever it holds, leads outside them.
+ * bf16: the softmax weights are rounded to bf16 for the product with v (their
+ * sum is that of the float32 weights). */
+typedef struct rtcc_attn_desc {
+    int32_t abi_version;          /* RTCC_ABI_VERSION                                   */
+    int32_t precision;            /* rtcc_precision of q, k, v, out                     */
+    int32_t n_seqs;               /* 0 .. 65536                                         */
+    int32_t q_heads, kv_heads;    /* 1 .. 1024; q_heads a multiple of kv_heads          */
+    int32_t head_dim;
+    int32_t causal;               /* 0 or 1                                             */
+    float scale;                  /* finite, > 0                                        */
+    float softcap;                /* finite, >= 0; 0: no cap                            */
+    int64_t q_rows;               /* rows of q and out; q_rows * q_heads < 2^31         */
+    int64_t k_rows;               /* rows of k and v, < 2^31                            */
+    const int32_t *q_offsets;     /* device [n_seqs + 1]                                */
+    const int32_t *k_offsets;     /* device [n_seqs], [n_seqs + 1] without k_lens       */
+    const int32_t *k_lens;        /* device [n_seqs] or NULL                            */
+    const int32_t *prefix_lens;   /* device [n_seqs] or NULL (0); causal = 1 only       */
+    const float *slopes;          /* device [q_heads] or NULL                           */
+    const void *q, *k, *v;
+    void *out;
+    int64_t q_stride[2], k_stride[2], v_stride[2], out_stride[2];
+    float *lse;                   /* device float32 [q_heads][q_rows] or NULL           */
+} rtcc_attn_desc;
+/* workspace: device memory of at least rtcc_attention_workspace bytes, 16-byte
+ * aligned (NULL where that is 0); it needs no initial contents. */
+RTCC_API rtcc_status rtcc_attention_workspace(const rtcc_attn_desc *desc, size_t *bytes);
+RTCC_API rtcc_status rtcc_attention(const rtcc_attn_desc *desc, void *workspace, size_t workspace_bytes,
+                                    void *hip_stream);
+
+/* Gradients of rtcc_attention with respect to q, k and v.  fwd describes the
+ * forward call whose out and lse (required) are read.  dout: as out.  dq, dk,
+ * dv: as q, k, v; written, not added to; dk and dv sum over the query heads of
+ * a key head, in a fixed order (the results of two calls are the same bits).
+ * Key ranges of different sequences must not overlap (their sums would race:
+ * undefined values).  Rows of q, k, v in no sequence are not written; a key
+ * that no query sees gets 0.  bf16: the softmax weights and their gradients
+ * are rounded to bf16 for the products. */
+typedef struct rtcc_attn_grad_desc {
+    rtcc_attn_desc fwd;
+    const void *dout;
+    void *dq, *dk, *dv;
+    int64_t dout_stride[2], dq_stride[2], dk_stride[2], dv_stride[2];
+} rtcc_attn_grad_desc;
+RTCC_API rtcc_status rtcc_attention_grad_workspace(const rtcc_attn_grad_desc *desc, size_t *bytes);
+RTCC_API rtcc_status rtcc_attention_grad(const rtcc_attn_grad_desc *desc, void *workspace, size_t workspace_bytes,
+                                         void *hip_stream);
+
+/* ------------------------------------------------------------------------
  * Host-side models of the communication and of the profiled DAG.  They run
  * on the host only (no GPU work, no context), are deterministic, and report
  * failures through rtcc_last_error(NULL).
@@ -602,8 +744,8 @@ RTCC_API rtcc_status rtcc_upward_rank(int32_t nodes, const int64_t *cost_ns, int
 RTCC_API const char *rtcc_status_str(rtcc_status s);
 
 /* Message of the last failed call on ctx; with ctx == NULL, the message of
- * the last failed context-free call (rtcc_create, rtcc_rotated_nms,
- * rtcc_uplink_emulate, rtcc_schedule_model, rtcc_upward_rank) on the
+ * the last failed context-free call (rtcc_create, rtcc_rotated_nms, the token
+ * operators, rtcc_uplink_emulate, rtcc_schedule_model, rtcc_upward_rank) on the
  * calling thread. */
 RTCC_API const char *rtcc_last_error(const rtcc_ctx *ctx);
 

@@ -16,6 +16,8 @@ Modules
   ofdma     the evaluation's OFDMA channel (mobility, path loss,
             blockage, fading), DAG upward rank and the paired
             measured-DAG trial in integer nanoseconds
+  tokens    norm and rotation of queries and keys, attention of packed
+            sequences, and the gradients of both
   nms       rotated bird's-eye-view IoU and greedy non-maximum suppression
 
 Parity status: every function is pinned by tests under ``tests/`` against

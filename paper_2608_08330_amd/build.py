@@ -25,7 +25,8 @@ ARCH = "gfx950"
 HIPCC = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
 CXX = shutil.which("g++") or "g++"
 
-HOST_SOURCES = ["api.cpp", "checkpoint.cpp", "controller.cpp", "model.cpp", "uplink.cpp", "kernels/conv_plan.cpp"]
+HOST_SOURCES = ["api.cpp", "checkpoint.cpp", "controller.cpp", "model.cpp", "uplink.cpp", "token_ops.cpp",
+                "kernels/conv_plan.cpp"]
 HIP_SOURCES = [
     "executor_hip.hip",
     "kernels/pillar.hip",
@@ -34,6 +35,9 @@ HIP_SOURCES = [
     "kernels/upsample.hip",
     "kernels/post.hip",
     "kernels/nms.hip",
+    "kernels/norm_rope.hip",
+    "kernels/attention.hip",
+    "kernels/attention_grad.hip",
     "nms_api.hip",
     "nms_noalloc.hip",
 ]

@@ -7,6 +7,7 @@
 #include <sstream>
 
 #include "controller.hpp"
+#include "kernels/token_ops.hpp"
 
 namespace rtcc {
 
@@ -171,3 +172,18 @@ extern "C" __attribute__((visibility("default"))) rtcc_status rtcc_rotated_nms_n
     rtcc::set_thread_error("rtcc_rotated_nms_noalloc needs the GPU library");
     return RTCC_E_STATE;
 }
+
+// The token operators' arguments are checked as in the GPU library; their
+// launchers then report that there is no GPU.
+namespace rtcc {
+namespace kern {
+size_t norm_rope_grad_workspace(const NormRopeArgs &) { return 0; }
+int norm_rope(const NormRopeArgs &, void *) { return -1; }
+int norm_rope_grad(const NormRopeArgs &, void *) { return -1; }
+size_t attention_workspace(const AttnArgs &) { return 0; }
+int attention(const AttnArgs &, void *) { return -1; }
+size_t attention_grad_workspace(const AttnArgs &) { return 0; }
+int attention_grad(const AttnArgs &, void *) { return -1; }
+const char *launch_error(int) { return nullptr; }
+}  // namespace kern
+}  // namespace rtcc

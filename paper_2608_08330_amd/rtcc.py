@@ -23,6 +23,7 @@ LIB_DIR = os.path.join(HERE, "lib")
 RTCC_ABI_VERSION = 6
 RTCC_MAX_AGENTS = 16
 RTCC_MAX_STAGES = 4
+RTCC_MAX_AXES = 3
 
 STATUS = {
     0: "RTCC_OK", 1: "RTCC_E_ARG", 2: "RTCC_E_STATE", 3: "RTCC_E_DUPLICATE",
@@ -169,11 +170,85 @@ class rtcc_detections(ctypes.Structure):
     ]
 
 
+_I64x2 = ctypes.c_int64 * 2
+
+
+class rtcc_norm_rope_desc(ctypes.Structure):
+    _fields_ = [
+        ("abi_version", ctypes.c_int32),
+        ("precision", ctypes.c_int32),
+        ("rows", ctypes.c_int64),
+        ("slot_rows", ctypes.c_int64),
+        ("q_heads", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("interleaved", ctypes.c_int32),
+        ("n_axes", ctypes.c_int32),
+        ("sections", ctypes.c_int32 * RTCC_MAX_AXES),
+        ("eps", ctypes.c_float),
+        ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("q_out", ctypes.c_void_p), ("k_out", ctypes.c_void_p), ("v_out", ctypes.c_void_p),
+        ("q_stride", _I64x2), ("k_stride", _I64x2), ("v_stride", _I64x2),
+        ("q_out_stride", _I64x2), ("k_out_stride", _I64x2), ("v_out_stride", _I64x2),
+        ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+        ("q_weight_per_head", ctypes.c_int32), ("k_weight_per_head", ctypes.c_int32),
+        ("positions", ctypes.c_void_p),
+        ("inv_freq", ctypes.c_void_p),
+        ("slots", ctypes.c_void_p),
+    ]
+
+
+class rtcc_norm_rope_grad_desc(ctypes.Structure):
+    _fields_ = [
+        ("fwd", rtcc_norm_rope_desc),
+        ("dq_out", ctypes.c_void_p), ("dk_out", ctypes.c_void_p),
+        ("dq", ctypes.c_void_p), ("dk", ctypes.c_void_p),
+        ("dq_out_stride", _I64x2), ("dk_out_stride", _I64x2), ("dq_stride", _I64x2), ("dk_stride", _I64x2),
+        ("dq_weight", ctypes.c_void_p), ("dk_weight", ctypes.c_void_p),
+    ]
+
+
+class rtcc_attn_desc(ctypes.Structure):
+    _fields_ = [
+        ("abi_version", ctypes.c_int32),
+        ("precision", ctypes.c_int32),
+        ("n_seqs", ctypes.c_int32),
+        ("q_heads", ctypes.c_int32),
+        ("kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("causal", ctypes.c_int32),
+        ("scale", ctypes.c_float),
+        ("softcap", ctypes.c_float),
+        ("q_rows", ctypes.c_int64),
+        ("k_rows", ctypes.c_int64),
+        ("q_offsets", ctypes.c_void_p),
+        ("k_offsets", ctypes.c_void_p),
+        ("k_lens", ctypes.c_void_p),
+        ("prefix_lens", ctypes.c_void_p),
+        ("slopes", ctypes.c_void_p),
+        ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+        ("out", ctypes.c_void_p),
+        ("q_stride", _I64x2), ("k_stride", _I64x2), ("v_stride", _I64x2), ("out_stride", _I64x2),
+        ("lse", ctypes.c_void_p),
+    ]
+
+
+class rtcc_attn_grad_desc(ctypes.Structure):
+    _fields_ = [
+        ("fwd", rtcc_attn_desc),
+        ("dout", ctypes.c_void_p),
+        ("dq", ctypes.c_void_p), ("dk", ctypes.c_void_p), ("dv", ctypes.c_void_p),
+        ("dout_stride", _I64x2), ("dq_stride", _I64x2), ("dk_stride", _I64x2), ("dv_stride", _I64x2),
+    ]
+
+
 EXPORTS = (
     "rtcc_create", "rtcc_read_checkpoint", "rtcc_create_from_checkpoint", "rtcc_destroy", "rtcc_set_mode", "rtcc_staging_buffer", "rtcc_begin_frame",
     "rtcc_release_branch", "rtcc_release_branch_device", "rtcc_release_branches", "rtcc_join_and_detect",
     "rtcc_get_branch_state", "rtcc_tensor_bytes", "rtcc_get_tensor", "rtcc_profile_nodes",
     "rtcc_node_times", "rtcc_node_count", "rtcc_graph_stats", "rtcc_conv_plan", "rtcc_conv_tiling", "rtcc_rotated_nms", "rtcc_rotated_nms_noalloc", "rtcc_uplink_emulate", "rtcc_schedule_model",
+    "rtcc_norm_rope", "rtcc_norm_rope_grad_workspace", "rtcc_norm_rope_grad",
+    "rtcc_attention_workspace", "rtcc_attention", "rtcc_attention_grad_workspace", "rtcc_attention_grad",
     "rtcc_upward_rank", "rtcc_status_str", "rtcc_last_error",
 )
 
@@ -219,6 +294,14 @@ def _declare(lib):
                                  ctypes.POINTER(ctypes.c_int64)]),
         "rtcc_rotated_nms_noalloc": (S, [_P, ctypes.c_int64, ctypes.c_int32, ctypes.c_float, _P,
                                          ctypes.POINTER(ctypes.c_int64), _P]),
+        "rtcc_norm_rope": (S, [ctypes.POINTER(rtcc_norm_rope_desc), _P]),
+        "rtcc_norm_rope_grad_workspace": (S, [ctypes.POINTER(rtcc_norm_rope_grad_desc),
+                                              ctypes.POINTER(ctypes.c_size_t)]),
+        "rtcc_norm_rope_grad": (S, [ctypes.POINTER(rtcc_norm_rope_grad_desc), _P, ctypes.c_size_t, _P]),
+        "rtcc_attention_workspace": (S, [ctypes.POINTER(rtcc_attn_desc), ctypes.POINTER(ctypes.c_size_t)]),
+        "rtcc_attention": (S, [ctypes.POINTER(rtcc_attn_desc), _P, ctypes.c_size_t, _P]),
+        "rtcc_attention_grad_workspace": (S, [ctypes.POINTER(rtcc_attn_grad_desc), ctypes.POINTER(ctypes.c_size_t)]),
+        "rtcc_attention_grad": (S, [ctypes.POINTER(rtcc_attn_grad_desc), _P, ctypes.c_size_t, _P]),
         "rtcc_uplink_emulate": (S, [ctypes.POINTER(rtcc_uplink_desc), _P, _P, _P, _P, _P]),
         "rtcc_schedule_model": (S, [ctypes.c_int32, _P, _P, ctypes.c_int64, ctypes.c_int32, _I64P, _I64P, _P]),
         "rtcc_upward_rank": (S, [ctypes.c_int32, _P, ctypes.c_int32, _P, _P]),
@@ -514,6 +597,200 @@ def rtcc_rotated_nms_noalloc(device_records, n, max_candidates, iou_threshold, d
     if st != 0:
         raise RtccError(st, (lib.rtcc_last_error(None) or b"").decode())
     return kept.value
+
+
+# ----------------------------------------------------------------------------
+# token operators
+# ----------------------------------------------------------------------------
+# The *_desc functions describe tensors (torch tensors, or anything with their
+# data_ptr(), stride(), shape and dtype): [rows, heads, head_dim], any row and
+# head strides the library takes.  A description holds addresses only; the
+# caller keeps the tensors.  The rtcc_* functions take a description, a
+# workspace address of the size their *_workspace function names, and a HIP
+# stream handle (integer, 0 = the null stream), and return once the work is
+# enqueued.
+
+_PRECISION = {"torch.float32": RTCC_PREC_FP32, "torch.bfloat16": RTCC_PREC_BF16}
+
+
+def _tokens(d, name, x, like=None):
+    """Fill the pointer and strides of tensor `name` of description d.
+    like: (shape, dtype) it has to have; None entries are free."""
+    if x.ndim != 3 or (x.shape[2] > 1 and x.stride(2) != 1):
+        raise ValueError("%s must be [rows, heads, head_dim] with contiguous heads" % name)
+    if like is not None:
+        if x.dtype != like[1]:
+            raise ValueError("%s must have dtype %s" % (name, like[1]))
+        if any(w is not None and w != g for w, g in zip(like[0], x.shape)):
+            raise ValueError("%s must have shape %s" % (name, tuple(like[0])))
+    s = x.stride()
+    setattr(d, name, x.data_ptr())
+    a = getattr(d, name + "_stride")
+    a[0], a[1] = s[0], s[1]
+
+
+def _flat(d, name, x, shape, dtype):
+    """Fill the pointer of a contiguous tensor of the given shape and dtype."""
+    if tuple(x.shape) != tuple(shape) or str(x.dtype) != dtype or not x.is_contiguous():
+        raise ValueError("%s must be a contiguous %s tensor of shape %s" % (name, dtype, tuple(shape)))
+    setattr(d, name, x.data_ptr())
+
+
+def _precision_of(x):
+    try:
+        return _PRECISION[str(x.dtype)]
+    except KeyError:
+        raise ValueError("the tensors must be float32 or bfloat16") from None
+
+
+def norm_rope_desc(q, k, q_out, k_out, q_weight, k_weight, positions, inv_freq, sections, eps=1e-6,
+                   interleaved=False, v=None, v_out=None, slots=None):
+    """Description of a norm and rotation of q and k (either may be None).
+    Weights: float32 [head_dim] or [heads, head_dim], or None.  positions
+    [rows, axes] and inv_freq [sum(sections)] float32.  With slots (int64
+    [rows]) k, and v if given, go to those rows of k_out and v_out."""
+    d = rtcc_norm_rope_desc()
+    x = q if q is not None else k
+    if x is None:
+        raise ValueError("q and k are both None")
+    rows, dim, dtype = x.shape[0], x.shape[2], x.dtype
+    d.abi_version, d.precision, d.rows, d.head_dim = RTCC_ABI_VERSION, _precision_of(x), rows, dim
+    d.interleaved, d.eps = int(bool(interleaved)), eps
+    d.n_axes = len(sections)
+    if not 1 <= len(sections) <= RTCC_MAX_AXES:
+        raise ValueError("sections must name 1 to %d axes" % RTCC_MAX_AXES)
+    d.sections[:len(sections)] = sections
+    if q is not None:
+        d.q_heads = q.shape[1]
+        _tokens(d, "q", q, ((rows, None, dim), dtype))
+        if q_out is not None:
+            _tokens(d, "q_out", q_out, (q.shape, dtype))
+    if k is not None:
+        d.kv_heads = k.shape[1]
+        _tokens(d, "k", k, ((rows, None, dim), dtype))
+        if k_out is not None:
+            _tokens(d, "k_out", k_out, ((rows if slots is None else None, k.shape[1], dim), dtype))
+    for name, w, heads in (("q_weight", q_weight, d.q_heads), ("k_weight", k_weight, d.kv_heads)):
+        if w is not None:
+            _flat(d, name, w, (dim,) if w.ndim == 1 else (heads, dim), "torch.float32")
+            if w.ndim == 2:
+                setattr(d, name + "_per_head", 1)
+    _flat(d, "positions", positions, (rows, len(sections)), "torch.float32")
+    _flat(d, "inv_freq", inv_freq, (sum(sections),), "torch.float32")
+    if slots is not None:
+        _flat(d, "slots", slots, (rows,), "torch.int64")
+        d.slot_rows = k_out.shape[0]
+    if v is not None:
+        _tokens(d, "v", v, (k.shape, dtype))
+        _tokens(d, "v_out", v_out, (k_out.shape, dtype))
+    return d
+
+
+def norm_rope_grad_desc(fwd, dq_out, dk_out, dq, dk, dq_weight=None, dk_weight=None):
+    """Description of the gradients of the call that fwd (norm_rope_desc)
+    describes; dq_weight and dk_weight: float32 of the weights' shapes."""
+    g = rtcc_norm_rope_grad_desc(fwd=fwd)
+    dtype = None
+    for names, heads in ((("dq_out", "dq"), fwd.q_heads), (("dk_out", "dk"), fwd.kv_heads)):
+        for name in names:
+            x = {"dq_out": dq_out, "dq": dq, "dk_out": dk_out, "dk": dk}[name]
+            if heads:
+                if _precision_of(x) != fwd.precision:
+                    raise ValueError("%s must have the forward tensors' dtype" % name)
+                dtype = x.dtype
+                _tokens(g, name, x, ((fwd.rows, heads, fwd.head_dim), dtype))
+    for name, w, heads, per_head in (("dq_weight", dq_weight, fwd.q_heads, fwd.q_weight_per_head),
+                                     ("dk_weight", dk_weight, fwd.kv_heads, fwd.k_weight_per_head)):
+        if w is not None:
+            _flat(g, name, w, (heads, fwd.head_dim) if per_head else (fwd.head_dim,), "torch.float32")
+    return g
+
+
+def attention_desc(q, k, v, out, q_offsets, k_offsets, k_lens=None, prefix_lens=None, slopes=None, lse=None,
+                   causal=False, scale=None, softcap=0.0):
+    """Description of an attention call: q, out [q_rows, q_heads, head_dim], k,
+    v [k_rows, kv_heads, head_dim]; q_offsets int32 [seqs + 1]; k_offsets int32
+    [seqs] with k_lens int32 [seqs], else [seqs + 1]; prefix_lens int32 [seqs];
+    slopes float32 [q_heads]; lse float32 [q_heads, q_rows].  scale: default
+    1 / sqrt(head_dim)."""
+    d = rtcc_attn_desc()
+    rows, heads, dim = q.shape
+    n = q_offsets.shape[0] - 1
+    d.abi_version, d.precision, d.n_seqs = RTCC_ABI_VERSION, _precision_of(q), n
+    d.q_heads, d.kv_heads, d.head_dim, d.causal = heads, k.shape[1], dim, int(bool(causal))
+    d.scale = dim ** -0.5 if scale is None else scale
+    d.softcap, d.q_rows, d.k_rows = softcap, rows, k.shape[0]
+    _flat(d, "q_offsets", q_offsets, (n + 1,), "torch.int32")
+    _flat(d, "k_offsets", k_offsets, (n if k_lens is not None else n + 1,), "torch.int32")
+    if k_lens is not None:
+        _flat(d, "k_lens", k_lens, (n,), "torch.int32")
+    if prefix_lens is not None:
+        _flat(d, "prefix_lens", prefix_lens, (n,), "torch.int32")
+    if slopes is not None:
+        _flat(d, "slopes", slopes, (heads,), "torch.float32")
+    if lse is not None:
+        _flat(d, "lse", lse, (heads, rows), "torch.float32")
+    dtype = q.dtype
+    _tokens(d, "q", q)
+    _tokens(d, "k", k, ((None, None, dim), dtype))
+    _tokens(d, "v", v, (k.shape, dtype))
+    _tokens(d, "out", out, (q.shape, dtype))
+    return d
+
+
+def attention_grad_desc(fwd, dout, dq, dk, dv):
+    """Description of the gradients of the call that fwd (attention_desc, with
+    its lse) describes."""
+    g = rtcc_attn_grad_desc(fwd=fwd)
+    if _precision_of(dout) != fwd.precision:
+        raise ValueError("dout must have the forward tensors' dtype")
+    for name, x, rows, heads in (("dout", dout, fwd.q_rows, fwd.q_heads), ("dq", dq, fwd.q_rows, fwd.q_heads),
+                                 ("dk", dk, fwd.k_rows, fwd.kv_heads), ("dv", dv, fwd.k_rows, fwd.kv_heads)):
+        _tokens(g, name, x, ((rows, heads, fwd.head_dim), dout.dtype))
+    return g
+
+
+def _workspace_call(fn, desc, kind):
+    lib = load(kind)
+    n = ctypes.c_size_t()
+    _free_call(lib, getattr(lib, fn)(ctypes.byref(desc), ctypes.byref(n)))
+    return n.value
+
+
+def rtcc_norm_rope(desc, stream=0, kind="gpu"):
+    """Norm and rotation of queries and keys (norm_rope_desc)."""
+    lib = load(kind)
+    _free_call(lib, lib.rtcc_norm_rope(ctypes.byref(desc), _P(stream)))
+
+
+def rtcc_norm_rope_grad_workspace(desc, kind="gpu"):
+    return _workspace_call("rtcc_norm_rope_grad_workspace", desc, kind)
+
+
+def rtcc_norm_rope_grad(desc, workspace, workspace_bytes, stream=0, kind="gpu"):
+    """Gradients of rtcc_norm_rope (norm_rope_grad_desc)."""
+    lib = load(kind)
+    _free_call(lib, lib.rtcc_norm_rope_grad(ctypes.byref(desc), _P(workspace), workspace_bytes, _P(stream)))
+
+
+def rtcc_attention_workspace(desc, kind="gpu"):
+    return _workspace_call("rtcc_attention_workspace", desc, kind)
+
+
+def rtcc_attention(desc, workspace, workspace_bytes, stream=0, kind="gpu"):
+    """Attention of packed sequences (attention_desc)."""
+    lib = load(kind)
+    _free_call(lib, lib.rtcc_attention(ctypes.byref(desc), _P(workspace), workspace_bytes, _P(stream)))
+
+
+def rtcc_attention_grad_workspace(desc, kind="gpu"):
+    return _workspace_call("rtcc_attention_grad_workspace", desc, kind)
+
+
+def rtcc_attention_grad(desc, workspace, workspace_bytes, stream=0, kind="gpu"):
+    """Gradients of rtcc_attention (attention_grad_desc)."""
+    lib = load(kind)
+    _free_call(lib, lib.rtcc_attention_grad(ctypes.byref(desc), _P(workspace), workspace_bytes, _P(stream)))
 
 
 def _free_call(lib, st):
