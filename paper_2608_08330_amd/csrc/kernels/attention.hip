@@ -65,8 +65,9 @@ struct Columns {
         l = 0.f;
     }
 
-    // Keys j0 .. j0 + 32 NB - 1 of the sequence, in LDS.
-    template <int NB>
+    // Keys j0 .. j0 + 32 NB - 1 of the sequence, in LDS; without MASK every
+    // column sees all of them.
+    template <int NB, bool MASK>
     __device__ void step(const AttnArgs &a, uint32_t kt, uint32_t vt, int j0) {
         f32x16_t x[NB];
 #pragma unroll
@@ -76,7 +77,6 @@ struct Columns {
             for (int kk = 0; kk < D / 16; ++kk)
                 x[b] = M::mma(L::row_frag(kt, b * 32 + (lane & 31), kk, h), q[kk], x[b]);
         }
-        const bool masked = j0 + 32 * NB > first_limit;  // wave-uniform
         if constexpr (CAP || BIAS) {
             const float away = place - float(j0) - 4.f * h;  // the distance to the half's first key
 #pragma unroll
@@ -91,7 +91,7 @@ struct Columns {
                 }
         }
         const float c1 = CAP || BIAS ? 1.f : score.c1;
-        if (masked) {
+        if constexpr (MASK) {
             const int left = limit - j0 - 4 * h;
 #pragma unroll
             for (int b = 0; b < NB; ++b)
@@ -137,7 +137,8 @@ struct Columns {
                 for (int e = 0; e < 8; ++e) v[e] = x[b][8 * s + e];
                 p[2 * b + s] = M::pack(v);
             }
-        Product<T, D, 2 * NB>::add(acc, p, vt, lane, masked && a.causal, [&](int j) { return j0 + j < limit; });
+        const bool look = MASK && a.causal && j0 + 32 * NB > first_limit;
+        Product<T, D, 2 * NB, MASK>::add(acc, p, vt, lane, look, [&](int j) { return j0 + j < limit; });
     }
 
     // Writes the columns: the result, or a share of it.
@@ -203,13 +204,27 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_tiles(AttnArgs 
         vs.load(v + int64_t(t) * N * a.v_s[0], keys - t * N, at + kBytes, threadIdx.x);
     };
     if (t0 < t1) load(t0, 0);
-    for (int t = t0; t < t1; ++t) {
+    int t = t0;
+    // pairs of tiles that every column of the block sees whole, each with the
+    // addresses of its buffer as constants
+    const int whole = min(t1, limit_of(a, sq, int(c0 / a.group)) / N);
+    for (; t + 2 <= whole; t += 2) {
+        wait_loads();
+        barrier();
+        load(t + 1, 1);
+        col.template step<N / 32, false>(a, base, base + kBytes, t * N);
+        wait_loads();
+        barrier();
+        if (t + 2 < t1) load(t + 2, 0);
+        col.template step<N / 32, false>(a, base + 2 * kBytes, base + 3 * kBytes, (t + 1) * N);
+    }
+    for (; t < t1; ++t) {
         const int buffer = (t - t0) & 1;
         wait_loads();
         barrier();
         if (t + 1 < t1) load(t + 1, buffer ^ 1);
         const uint32_t at = base + buffer * 2 * kBytes;
-        if (t * N < col.last_limit) col.template step<N / 32>(a, at, at + kBytes, t * N);
+        if (t * N < col.last_limit) col.template step<N / 32, true>(a, at, at + kBytes, t * N);
     }
     col.store(a, sh, blockIdx.y);
 }
@@ -257,7 +272,8 @@ __global__ __launch_bounds__((64 * kFewWaves<T, D>), 1) void k_few(AttnArgs a, i
             wait_loads();
         }
         const uint32_t at = base + buffer * 2 * kBytes;
-        col.template step<1>(a, at, at + kBytes, t * N);
+        if ((t + 1) * N <= col.first_limit) col.template step<1, false>(a, at, at + kBytes, t * N);
+        else col.template step<1, true>(a, at, at + kBytes, t * N);
     }
 
     // join the waves: [wave][column] maximum and sum, then the outputs

@@ -300,9 +300,10 @@ __device__ inline int limit_of(const AttnArgs &a, const Seq &q, int i) {
 
 // Products of a tile's columns with weights: acc[t] += tile[:, 32 t ..]^T w, the
 // weights of 16 tile rows a step.  A weight of 0 times a value that is not
-// finite would still reach the sum; with `look`, rows that hold such values
-// are taken one by one, for the lanes (columns of the result) that see them.
-template <typename T, int D, int STEPS>
+// finite would still reach the sum; with `look` (where MASK allows it), rows
+// that hold such values are taken one by one, for the lanes (columns of the
+// result) that see them.
+template <typename T, int D, int STEPS, bool MASK>
 struct Product {
     typedef Op<T> M;
     typedef Tile<T, D> L;
@@ -310,7 +311,7 @@ struct Product {
     template <typename SEEN>
     __device__ static void add(f32x16_t *acc, const typename M::Frag *w, uint32_t tile, int lane, bool look,
                                const SEEN &seen) {
-        if (look) {
+        if (MASK && look) {
             const unsigned long long bad = not_finite(tile, lane);
             if (bad) {
                 apart(acc, w, tile, lane, bad, seen);

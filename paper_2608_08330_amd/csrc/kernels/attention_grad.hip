@@ -154,7 +154,7 @@ __global__ __launch_bounds__(256, (kWavesDq<T, D>)) void k_dq(AttnArgs a, int ti
                 ds[r] = d;
             }
             typename M::Frag w[2] = {M::pack(ds), M::pack(ds + 8)};
-            Product<T, D, 2>::add(acc, w, kb, lane, masked && a.causal, [&](int j) { return j0 + j < limit; });
+            Product<T, D, 2, true>::add(acc, w, kb, lane, masked && a.causal, [&](int j) { return j0 + j < limit; });
         }
     }
     if (!at.valid) return;
@@ -277,10 +277,10 @@ __global__ __launch_bounds__(256, (kWavesDkv<T, D>)) void k_dkv(AttnArgs a, int 
             auto seen = [&](int r) { return r >= hidden; };
             const bool look = masked && a.causal;
             typename M::Frag w[2] = {M::pack(p), M::pack(p + 8)};
-            Product<T, D, 2>::add(dv, w, gb, lane, look, seen);
+            Product<T, D, 2, true>::add(dv, w, gb, lane, look, seen);
             w[0] = M::pack(ds);
             w[1] = M::pack(ds + 8);
-            Product<T, D, 2>::add(dk, w, qb, lane, look, seen);
+            Product<T, D, 2, true>::add(dk, w, qb, lane, look, seen);
         }
         if (++now_qt == per_head) now_qt = 0, ++now_head;
         if (u + 1 < n) put(buffer ^ 1);
