@@ -10,13 +10,16 @@
 // (attention.hpp), and the output is accumulated transposed, V^T P^T.
 //
 //   tiles: four waves x 32 columns walk the keys together, K and V staged
-//     straight into LDS, two buffers, one barrier a tile.
+//     straight into LDS, two buffers, one barrier a tile.  Tiles that all
+//     columns see whole run in turns (bf16): the products of the next tile and
+//     of the last beside the softmax of this one.
 //   few:   for sequences of few columns (single tokens): the waves of a block
 //     share 32 columns and walk tiles of 32 keys of their own, each through
 //     its own LDS, without a barrier; their results are joined in LDS.
 // Both take a share of a sequence's keys where whole sequences would leave
 // compute units idle; `join` then adds the shares up in a fixed order.
 #include <algorithm>
+#include <type_traits>
 
 #include "attention.hpp"
 #include "compute_units.hpp"
@@ -63,73 +66,69 @@ struct Columns {
         for (int t = 0; t < D / 32; ++t) acc[t] = f32x16_t{};
         m = -kInf;
         l = 0.f;
+        wait_registers();
     }
 
-    // Keys j0 .. j0 + 32 NB - 1 of the sequence, in LDS; without MASK every
-    // column sees all of them.
-    template <int NB, bool MASK>
-    __device__ void step(const AttnArgs &a, uint32_t kt, uint32_t vt, int j0) {
-        f32x16_t x[NB];
+    // Products <k, q> of the keys in a tile.
+    template <int NB>
+    __device__ void products(f32x16_t *x, uint32_t kt) const {
 #pragma unroll
-        for (int b = 0; b < NB; ++b) {
-            x[b] = f32x16_t{};
+        for (int b = 0; b < NB; ++b) x[b] = f32x16_t{};
 #pragma unroll
-            for (int kk = 0; kk < D / 16; ++kk)
-                x[b] = M::mma(L::row_frag(kt, b * 32 + (lane & 31), kk, h), q[kk], x[b]);
-        }
-        if constexpr (CAP || BIAS) {
-            const float away = place - float(j0) - 4.f * h;  // the distance to the half's first key
+        for (int kk = 0; kk < D / 16; ++kk)
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    float y = x[b][r];
-                    if constexpr (CAP) y = score.capl * score.tanh_of(y);
-                    else y *= score.c1;
-                    if constexpr (BIAS) y = fmaf(-slope, fabsf(away - float(b * 32 + 8 * (r >> 2) + (r & 3))), y);
-                    x[b][r] = y;
-                }
-        }
-        const float c1 = CAP || BIAS ? 1.f : score.c1;
-        if constexpr (MASK) {
-            const int left = limit - j0 - 4 * h;
-#pragma unroll
-            for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (b * 32 + 8 * (r >> 2) + (r & 3) >= left) x[b][r] = -kInf;
-        }
-        float top = x[0][0];
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, x[b][r]);
-        top = half_max(top) * c1;
-        // The running maximum follows only where it is left behind by more
-        // than 2^8 (any value will do while the weights stay in range): the
-        // output is rescaled a few times a row instead of once a tile.
-        if (__any(top > m + 8.f)) {
-            const float now = fmaxf(m, top);
-            const float f = m == -kInf ? 0.f : __builtin_amdgcn_exp2f(m - now);
-            m = now;
-            l *= f;
-#pragma unroll
-            for (int t = 0; t < D / 32; ++t) acc[t] *= f;
-        }
-        const float base = m == -kInf ? 0.f : m;
-        float sum = 0.f;
+            for (int b = 0; b < NB; ++b) x[b] = M::mma(L::row_frag(kt, b * 32 + (lane & 31), kk, h), q[kk], x[b]);
+    }
+
+    // One score from its product; `key` is counted from the half's first key,
+    // `away` the query's distance to that.
+    __device__ float scored(float x, int key, float away) const {
+        if constexpr (CAP) x = score.capl * score.tanh_of(x);
+        else if constexpr (BIAS) x *= score.c1;
+        if constexpr (BIAS) x = fmaf(-slope, fabsf(away - float(key)), x);
+        return x;
+    }
+    // What is left to multiply scores by.
+    __device__ float factor() const { return CAP || BIAS ? 1.f : score.c1; }
+
+    // Advances the running maximum past `top`, a tile's own in this half.  It
+    // follows only where it is left behind by more than 2^8 (any value will do
+    // while the weights stay in range), so that the output is rescaled a few
+    // times a row instead of once a tile.  base: what to subtract from
+    // scores; returns the factor of the sums so far.
+    __device__ float advance(float top, float &base) {
+        top = half_max(top) * factor();
+        const float before = m;
+        m = top > m + 8.f ? top : m;
+        base = m == -kInf ? 0.f : m;
+        return __builtin_amdgcn_exp2f(before - base);
+    }
+
+    // The weights of the keys from j0 on, from their products x, as operands;
+    // advances the maximum and the sum.  Returns what the output so far is to
+    // be multiplied by.
+    template <int NB>
+    __device__ float weights(f32x16_t *x, typename M::Frag *p, int j0) {
+        const float away = place - float(j0) - 4.f * h;
+        const int left = limit - j0 - 4 * h;
+        float top = -kInf;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const float p = __builtin_amdgcn_exp2f(fmaf(x[b][r], c1, -base));
-                x[b][r] = p;
-                sum += p;
+                const int key = b * 32 + 8 * (r >> 2) + (r & 3);
+                x[b][r] = key < left ? scored(x[b][r], key, away) : -kInf;
+                top = fmaxf(top, x[b][r]);
             }
-        l += sum;
-        typename M::Frag p[2 * NB];
+        float base, sum = 0.f;
+        const float f = advance(top, base);
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+        for (int b = 0; b < NB; ++b) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                x[b][r] = __builtin_amdgcn_exp2f(fmaf(x[b][r], factor(), -base));
+                sum += x[b][r];
+            }
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 float v[8];
@@ -137,8 +136,28 @@ struct Columns {
                 for (int e = 0; e < 8; ++e) v[e] = x[b][8 * s + e];
                 p[2 * b + s] = M::pack(v);
             }
-        const bool look = MASK && a.causal && j0 + 32 * NB > first_limit;
-        Product<T, D, 2 * NB, MASK>::add(acc, p, vt, lane, look, [&](int j) { return j0 + j < limit; });
+        }
+        l = fmaf(l, f, sum);
+        return f;
+    }
+
+    // f may be anything where there is nothing to multiply yet
+    __device__ void rescale(float f) {
+        if (__any(f != 1.f)) {
+#pragma unroll
+            for (int t = 0; t < D / 32; ++t) acc[t] *= f;
+        }
+    }
+
+    // One tile, keys j0 .. j0 + 32 NB - 1 of the sequence, part after part.
+    template <int NB>
+    __device__ void step(const AttnArgs &a, uint32_t kt, uint32_t vt, int j0) {
+        f32x16_t x[NB];
+        typename M::Frag p[2 * NB];
+        products<NB>(x, kt);
+        rescale(weights<NB>(x, p, j0));
+        const bool look = a.causal && j0 + 32 * NB > first_limit;
+        Product<T, D, 2 * NB, true>::add(acc, p, vt, lane, look, [&](int j) { return j0 + j < limit; });
     }
 
     // Writes the columns: the result, or a share of it.
@@ -168,12 +187,15 @@ __device__ inline void share(int n, int splits, int i, int least, int &first, in
 }
 
 constexpr int kTileColumns = 128, kFewColumns = 32, kJoinColumns = 16;
-constexpr int kTileKeys(bool bf16) { return bf16 ? 64 : 32; }
-constexpr int kLeastShare = 4;  // tiles: 256 keys, or 128
+// Keys of a tile of `tiles`.
+template <typename T, int D>
+constexpr int kTileKeys = sizeof(T) == 2 && D <= 64 ? 64 : 32;
+constexpr int kLeastShare = 128;  // keys
+
 
 template <typename T, int D, bool CAP, bool BIAS>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_tiles(AttnArgs a, int tiles, Shares sh) {
-    constexpr int N = kTileKeys(sizeof(T) == 2);
+    constexpr int N = kTileKeys<T, D>;
     constexpr uint32_t kBytes = N * Tile<T, D>::kRowBytes;
     extern __shared__ __align__(1024) unsigned char lds[];
     const int id = spread(blockIdx.x, gridDim.x);
@@ -190,7 +212,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_tiles(AttnArgs 
     const int64_t c_last = min(c0 + kTileColumns, columns) - 1;
     const int keys = limit_of(a, sq, int(c_last / a.group));
     int t0, t1;
-    share((keys + N - 1) / N, sh.splits, blockIdx.y, kLeastShare, t0, t1);
+    share((keys + N - 1) / N, sh.splits, blockIdx.y, kLeastShare / N, t0, t1);
 
     const T *k = static_cast<const T *>(a.k) + sq.k0 * a.k_s[0] + kvh * a.k_s[1];
     const T *v = static_cast<const T *>(a.v) + sq.k0 * a.v_s[0] + kvh * a.v_s[1];
@@ -198,33 +220,124 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_tiles(AttnArgs 
     ks.init(threadIdx.x, a.k_s[0], a.dim);
     vs.init(threadIdx.x, a.v_s[0], a.dim);
     const uint32_t base = lds_offset(lds);
-    auto load = [&](int t, int buffer) {
-        const uint32_t at = base + buffer * 2 * kBytes;
-        ks.load(k + int64_t(t) * N * a.k_s[0], keys - t * N, at, threadIdx.x);
-        vs.load(v + int64_t(t) * N * a.v_s[0], keys - t * N, at + kBytes, threadIdx.x);
+    // buffers: K 0, K 1, V 0, V 1
+    auto load_k = [&](int t, int buffer) {
+        ks.load(k + int64_t(t) * N * a.k_s[0], keys - t * N, base + buffer * kBytes, threadIdx.x);
     };
-    if (t0 < t1) load(t0, 0);
+    auto load_v = [&](int t, int buffer) {
+        vs.load(v + int64_t(t) * N * a.v_s[0], keys - t * N, base + (2 + buffer) * kBytes, threadIdx.x);
+    };
+    constexpr int NB = N / 32;
     int t = t0;
-    // pairs of tiles that every column of the block sees whole, each with the
-    // addresses of its buffer as constants
-    const int whole = min(t1, limit_of(a, sq, int(c0 / a.group)) / N);
-    for (; t + 2 <= whole; t += 2) {
-        wait_loads();
-        barrier();
-        load(t + 1, 1);
-        col.template step<N / 32, false>(a, base, base + kBytes, t * N);
-        wait_loads();
-        barrier();
-        if (t + 2 < t1) load(t + 2, 0);
-        col.template step<N / 32, false>(a, base + 2 * kBytes, base + 3 * kBytes, (t + 1) * N);
+    // Tiles that every column of the block sees whole, an even number of them,
+    // in turns that run three tiles at once: the products of the next, the
+    // weights of this one and the output of the last, so that the matrix cores
+    // and the vector units have independent work from one wave.
+    const int whole = max(0, min(t1, limit_of(a, sq, int(c0 / a.group)) / N) - t0) & ~1;
+    if constexpr (sizeof(T) == 2) {
+        // base is 0: the block's only LDS is this
+        f32x16_t x0[NB], x1[NB];
+        bf16x8_t p0[2 * NB] = {}, p1[2 * NB] = {};
+        Lanes<D> at;
+        Walk<Stager<T, D, N, 256>, N> kw, vw;
+        at.init(col.lane);
+        auto turn = [&](f32x16_t *x, f32x16_t *next, bf16x8_t *p, bf16x8_t *last, int now, auto which) {
+            constexpr int buffer = decltype(which)::value, other = buffer ^ 1;
+            wait_loads();
+            barrier();
+            if (now + 2 < t0 + whole) kw.template load<buffer * kBytes>(ks);
+            vw.template load<(2 + buffer) * kBytes>(vs);
+            // H products of the next tile and H of the last, a share of this
+            // tile's vector work after each; reads from LDS run ahead
+            constexpr int H = NB * D / 16, E = NB * 16, W = D / 32;
+            constexpr int kAhead = H < 4 ? H : 4;
+            bf16x8_t f[2 * H];
+            auto read = [&](int i) {
+                f[i] = i < H ? at.row_frag(other * kBytes, i % NB, i / NB)
+                             : at.col_frag((2 + other) * kBytes, (i - H) / W, (i - H) % W);
+            };
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) read(i);
+            __builtin_amdgcn_sched_barrier(0);
+            const float away = col.place - float(now * N) - 4.f * col.h;
+            float top = -kInf, base = 0.f, less = 1.f, sum = 0.f;
+            // plain scores: the maximum first, the weights beside all products;
+            // others: the scores beside the first half, the weights beside the
+            // second
+            auto raise = [&](int e) {
+                const float y = col.scored(x[e / 16][e % 16], e / 16 * 32 + 8 * (e % 16 >> 2) + (e & 3), away);
+                x[e / 16][e % 16] = y;
+                top = fmaxf(top, y);
+            };
+            uint32_t words[E / 2];
+            float even = 0.f;
+            auto weigh = [&](int e) {
+                const float w = __builtin_amdgcn_exp2f(fmaf(x[e / 16][e % 16], col.factor(), -base));
+                sum += w;
+                const bf16x2_t two = {__bf16(even), __bf16(w)};
+                if (e % 2) words[e / 2] = Lanes<D>::opaque(__builtin_bit_cast(uint32_t, two));
+                even = w;
+            };
+            if constexpr (!CAP && !BIAS) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) raise(e);
+                less = col.advance(top, base);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int b = 0; b < NB; ++b) next[b] = f32x16_t{};
+#pragma unroll
+            for (int i = 0; i < 2 * H; ++i) {
+                if (i < H) next[i % NB] = Op<T>::mma(f[i], col.q[i / NB], next[i % NB]);
+                else col.acc[(i - H) % W] = Op<T>::mma(f[i], last[(i - H) / W], col.acc[(i - H) % W]);
+                if (i + kAhead < 2 * H) read(i + kAhead);
+                if constexpr (!CAP && !BIAS) {
+#pragma unroll
+                    for (int e = i * E / (2 * H); e < (i + 1) * E / (2 * H); ++e) weigh(e);
+                } else {
+#pragma unroll
+                    for (int e = i % H * E / H; e < (i % H + 1) * E / H; ++e) {
+                        if (i < H) raise(e);
+                        else weigh(e);
+                    }
+                    if (i == H - 1) less = col.advance(top, base);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int i = 0; i < 2 * NB; ++i) {
+                const u32x4_t u = {words[4 * i], words[4 * i + 1], words[4 * i + 2], words[4 * i + 3]};
+                p[i] = __builtin_bit_cast(bf16x8_t, u);
+            }
+            col.l = fmaf(col.l, less, sum);
+            col.rescale(less);
+        };
+        if (whole > 0) {
+            kw.init(ks, k + int64_t(t) * N * a.k_s[0], threadIdx.x);
+            vw.init(vs, v + int64_t(t) * N * a.v_s[0], threadIdx.x);
+            kw.template load<0>(ks);
+            vs.load(v, 0, base + 3 * kBytes, threadIdx.x);  // zeros, the values of a tile before the first
+            wait_loads();
+            barrier();
+            kw.template load<kBytes>(ks);
+            col.template products<NB>(x0, base);
+            for (; t < t0 + whole; t += 2) {
+                turn(x0, x1, p0, p1, t, std::integral_constant<int, 0>());
+                turn(x1, x0, p1, p0, t + 1, std::integral_constant<int, 1>());
+            }
+            wait_loads();
+            barrier();
+            Product<T, D, 2 * NB, false>::add(col.acc, p1, base + 3 * kBytes, col.lane, false, [](int) { return true; });
+            barrier();
+        }
     }
-    for (; t < t1; ++t) {
-        const int buffer = (t - t0) & 1;
+    if (t < t1) load_k(t, 0), load_v(t, 0);
+    for (int buffer = 0; t < t1; ++t, buffer ^= 1) {
         wait_loads();
         barrier();
-        if (t + 1 < t1) load(t + 1, buffer ^ 1);
-        const uint32_t at = base + buffer * 2 * kBytes;
-        if (t * N < col.last_limit) col.template step<N / 32, true>(a, at, at + kBytes, t * N);
+        if (t + 1 < t1) load_k(t + 1, buffer ^ 1), load_v(t + 1, buffer ^ 1);
+        if (t * N < col.last_limit)
+            col.template step<NB>(a, base + buffer * kBytes, base + (2 + buffer) * kBytes, t * N);
     }
     col.store(a, sh, blockIdx.y);
 }
@@ -248,7 +361,7 @@ __global__ __launch_bounds__((64 * kFewWaves<T, D>), 1) void k_few(AttnArgs a, i
     col.init(a, sq, kvh, c0);
     const int keys = col.last_limit;
     int t0, t1;
-    share((keys + N - 1) / N, sh.splits, blockIdx.y, kLeastShare * W, t0, t1);
+    share((keys + N - 1) / N, sh.splits, blockIdx.y, kLeastShare / N * W, t0, t1);
 
     const T *k = static_cast<const T *>(a.k) + sq.k0 * a.k_s[0] + kvh * a.k_s[1];
     const T *v = static_cast<const T *>(a.v) + sq.k0 * a.v_s[0] + kvh * a.v_s[1];
@@ -272,8 +385,7 @@ __global__ __launch_bounds__((64 * kFewWaves<T, D>), 1) void k_few(AttnArgs a, i
             wait_loads();
         }
         const uint32_t at = base + buffer * 2 * kBytes;
-        if ((t + 1) * N <= col.first_limit) col.template step<1, false>(a, at, at + kBytes, t * N);
-        else col.template step<1, true>(a, at, at + kBytes, t * N);
+        col.template step<1>(a, at, at + kBytes, t * N);
     }
 
     // join the waves: [wave][column] maximum and sum, then the outputs
@@ -409,7 +521,7 @@ hipError_t run(const AttnArgs &a, const Plan &p, hipStream_t s) {
         if (e != hipSuccess) return e;
         k_few<T, D, CAP, BIAS><<<grid, 64 * W, lds, s>>>(a, p.tiles, sh);
     } else {
-        constexpr int lds = 4 * kTileKeys(sizeof(T) == 2) * Tile<T, D>::kRowBytes;
+        constexpr int lds = 4 * kTileKeys<T, D> * Tile<T, D>::kRowBytes;
         const hipError_t e = max_lds(k_tiles<T, D, CAP, BIAS>, lds);
         if (e != hipSuccess) return e;
         k_tiles<T, D, CAP, BIAS><<<grid, 256, lds, s>>>(a, p.tiles, sh);

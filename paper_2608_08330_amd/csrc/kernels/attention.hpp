@@ -119,6 +119,20 @@ struct Tile {
         }
     }
 
+    // Channels d .. d + 3 of row r, d a multiple of 4.
+    __device__ static void four(uint32_t tile, uint32_t r, uint32_t d, float *v) {
+        const uint32_t b = d * sizeof(T), at = tile + r * kRowBytes + (((b >> 4) ^ turn(r)) << 4) + (b & 15);
+        if constexpr (sizeof(T) == 2) {
+            const s16x4_t u = *(lds_s16x4 *)at;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(uint32_t(uint16_t(u[e])) << 16);
+        } else {
+            const u32x4_t u = *(lds_u32x4 *)at;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(u[e]);
+        }
+    }
+
     // Operand with columns 32 dt .. of the tile as its rows and tile rows as
     // the contracted values: rows 16 s + 4 h + e (e < 4), 16 s + 8 + 4 h + e - 4.
     __device__ static typename Op<T>::Frag col_frag(uint32_t tile, int s, int dt, int lane) {
@@ -145,6 +159,39 @@ struct Tile {
             }
             return f;
         }
+    }
+};
+
+// A lane's addresses in a tile at LDS address 0, for reads of many tiles: the
+// rest of an address is a constant of the instruction.
+template <int D>
+struct Lanes {
+    typedef Tile<uint16_t, D> L;
+    uint32_t row[D / 16], col[D / 32][2];
+    __device__ void init(int lane) {
+        const uint32_t h = lane >> 5, r = lane & 31, rc = 4 * h + ((lane & 15) >> 2);
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) row[kk] = opaque(r * L::kRowBytes + (((2 * kk + h) ^ L::turn(r)) << 4));
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t) {
+            const uint32_t c = t * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), at = rc * L::kRowBytes + (lane & 1) * 8;
+            col[t][0] = opaque(at + ((c ^ L::turn(rc)) << 4));
+            col[t][1] = opaque(at + 8 * L::kRowBytes + ((c ^ L::turn(rc + 8)) << 4));
+        }
+    }
+    // Tile::row_frag of row 32 b + lane % 32, and Tile::col_frag
+    __device__ bf16x8_t row_frag(uint32_t tile, int b, int kk) const {
+        return __builtin_bit_cast(bf16x8_t, *(lds_u32x4 *)(row[kk] + (tile + b * 32 * L::kRowBytes)));
+    }
+    __device__ bf16x8_t col_frag(uint32_t tile, int s, int t) const {
+        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(col[t][0] + (tile + 16 * s * L::kRowBytes)));
+        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(col[t][1] + (tile + 16 * s * L::kRowBytes)));
+        return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    // not to be computed again at its uses
+    __device__ static uint32_t opaque(uint32_t x) {
+        asm volatile("" : "+v"(x));
+        return x;
     }
 };
 
@@ -213,12 +260,50 @@ struct Stager {
     }
 };
 
+// A Stager's tiles one after another, all of them whole: the scalar work of a
+// tile is one addition.
+template <typename S, int ROWS>
+struct Walk {
+    u32x4_t rsrc;
+    uint64_t step;
+    uint32_t at;  // the wave's part of a tile at LDS address 0
+    template <typename T>
+    __device__ void init(const S &s, const T *src, int thread) {
+        const uint64_t p = reinterpret_cast<uint64_t>(src);
+        rsrc[0] = __builtin_amdgcn_readfirstlane(uint32_t(p));
+        rsrc[1] = __builtin_amdgcn_readfirstlane(uint32_t(p >> 32) & 0xffffu);
+        rsrc[2] = __builtin_amdgcn_readfirstlane(uint32_t(ROWS - 1) * s.row_bytes + s.head_bytes);
+        rsrc[3] = 0x00020000u;
+        const uint64_t bytes = uint64_t(ROWS) * s.row_bytes;
+        step = uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(bytes >> 32))) << 32 |
+               __builtin_amdgcn_readfirstlane(uint32_t(bytes));
+        at = __builtin_amdgcn_readfirstlane(uint32_t(thread >> 6) * (S::kLoads * 1024));
+    }
+    // The next tile, to LDS address TO.
+    template <uint32_t TO>
+    __device__ void load(const S &s) {
+#pragma unroll
+        for (int n = 0; n < S::kLoads; ++n) {
+            asm volatile("s_add_u32 m0, %2, %3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(s.off[n]), "s"(rsrc),
+                         "s"(at), "i"(TO + uint32_t(n) * 1024)
+                         : "memory", "m0", "scc");
+        }
+        const uint64_t p = (uint64_t(rsrc[1]) << 32 | rsrc[0]) + step;
+        rsrc[0] = uint32_t(p);
+        rsrc[1] = uint32_t(p >> 32);
+    }
+};
+
 // All direct loads of this wave have arrived.
 __device__ inline void wait_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 template <int N>
 __device__ inline void wait_loads_but() {
     asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
+// Registers loaded from global memory have arrived.  Said to the compiler: it
+// cannot count the direct loads, and a register load that it still takes to be
+// on its way where a loop begins costs a wait for all of them in every turn.
+__device__ inline void wait_registers() { __builtin_amdgcn_s_waitcnt(0x0f70); }  // vmcnt(0) alone
 // This wave's reads of a tile are done: direct loads may write over it.
 __device__ inline void wait_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 __device__ inline void barrier() {
@@ -351,18 +436,31 @@ struct Product {
                 acc[t] = M::mma(only(L::col_frag(tile, s, t, lane), s, lane, ~bad), w[s], acc[t]);
 #pragma unroll 1
         for (; bad; bad &= bad - 1) {
-            const int j = __builtin_ctzll(bad);
+            const int j = __builtin_ctzll(bad), h = lane >> 5;
+            const float f = weight(w, j, h);
             const bool see = seen(j);
 #pragma unroll
-            for (int t = 0; t < D / 32; ++t) {
-                f32x16_t with = acc[t];
+            for (int t = 0; t < D / 32; ++t)
 #pragma unroll
-                for (int s = 0; s < STEPS; ++s)
-                    with = M::mma(only(L::col_frag(tile, s, t, lane), s, lane, 1ull << j), w[s], with);
+                for (int g = 0; g < 4; ++g) {
+                    float v[4];
+                    L::four(tile, j, 32 * t + 8 * g + 4 * h, v);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) acc[t][r] = see ? with[r] : acc[t][r];
-            }
+                    for (int e = 0; e < 4; ++e) acc[t][4 * g + e] = see ? fmaf(f, v[e], acc[t][4 * g + e]) : acc[t][4 * g + e];
+                }
         }
+    }
+    // The weight of tile row j in the lane's column.
+    __device__ static float weight(const typename M::Frag *w, int j, int h) {
+        const int step = j >> 4, place = (j >> 3 & 1) * 4 + (j & 3);
+        float f = 0.f;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (s == step && e == place) f = M::widen(w[s], e);
+        const float other = other_half(f, h != 0);
+        return (j >> 2 & 1) == h ? f : other;
     }
     __device__ static typename M::Frag only(typename M::Frag f, int s, int lane, unsigned long long keep) {
 #pragma unroll
