@@ -194,14 +194,13 @@ constexpr int kLeastShare = 128;  // keys
 
 
 template <typename T, int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_tiles(AttnArgs a, int tiles, Shares sh) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_tiles(AttnArgs a, Shares sh) {
     constexpr int N = kTileKeys<T, D>;
     constexpr uint32_t kBytes = N * Tile<T, D>::kRowBytes;
     extern __shared__ __align__(1024) unsigned char lds[];
-    const int id = spread(blockIdx.x, gridDim.x);
     Seq sq;
-    if (!find_tile<false>(a, id % tiles, kTileColumns, sq)) return;
-    const int kvh = id / tiles, wave = threadIdx.x >> 6;
+    if (!find_tile<false>(a, tile_of(a), kTileColumns, sq)) return;
+    const int kvh = head_of(a), wave = threadIdx.x >> 6;
     const int64_t columns = int64_t(sq.nq) * a.group;
     // the last tiles of a causal sequence have the most keys: first
     const int mine = a.causal ? int((columns + kTileColumns - 1) / kTileColumns) - 1 - sq.tile : sq.tile;
@@ -235,12 +234,11 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_tiles(AttnArgs 
     // and the vector units have independent work from one wave.
     const int whole = max(0, min(t1, limit_of(a, sq, int(c0 / a.group)) / N) - t0) & ~1;
     if constexpr (sizeof(T) == 2) {
-        // base is 0: the block's only LDS is this
         f32x16_t x0[NB], x1[NB];
         bf16x8_t p0[2 * NB] = {}, p1[2 * NB] = {};
-        Lanes<D> at;
+        Lanes<T, D> at;
         Walk<Stager<T, D, N, 256>, N> kw, vw;
-        at.init(col.lane);
+        at.init(col.lane, base);
         auto turn = [&](f32x16_t *x, f32x16_t *next, bf16x8_t *p, bf16x8_t *last, int now, auto which) {
             constexpr int buffer = decltype(which)::value, other = buffer ^ 1;
             wait_loads();
@@ -275,7 +273,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_tiles(AttnArgs 
                 const float w = __builtin_amdgcn_exp2f(fmaf(x[e / 16][e % 16], col.factor(), -base));
                 sum += w;
                 const bf16x2_t two = {__bf16(even), __bf16(w)};
-                if (e % 2) words[e / 2] = Lanes<D>::opaque(__builtin_bit_cast(uint32_t, two));
+                if (e % 2) words[e / 2] = Lanes<T, D>::opaque(__builtin_bit_cast(uint32_t, two));
                 even = w;
             };
             if constexpr (!CAP && !BIAS) {
@@ -313,8 +311,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_tiles(AttnArgs 
             col.rescale(less);
         };
         if (whole > 0) {
-            kw.init(ks, k + int64_t(t) * N * a.k_s[0], threadIdx.x);
-            vw.init(vs, v + int64_t(t) * N * a.v_s[0], threadIdx.x);
+            kw.init(ks, k + int64_t(t) * N * a.k_s[0], threadIdx.x, base);
+            vw.init(vs, v + int64_t(t) * N * a.v_s[0], threadIdx.x, base);
             kw.template load<0>(ks);
             vs.load(v, 0, base + 3 * kBytes, threadIdx.x);  // zeros, the values of a tile before the first
             wait_loads();
@@ -347,14 +345,13 @@ template <typename T, int D>
 constexpr int kFewWaves = sizeof(T) == 4 && D == 128 ? 2 : 4;
 
 template <typename T, int D, bool CAP, bool BIAS>
-__global__ __launch_bounds__((64 * kFewWaves<T, D>), 1) void k_few(AttnArgs a, int tiles, Shares sh) {
+__global__ __launch_bounds__((64 * kFewWaves<T, D>), 1) void k_few(AttnArgs a, Shares sh) {
     constexpr int W = kFewWaves<T, D>, N = 32;
     constexpr uint32_t kBytes = N * Tile<T, D>::kRowBytes;
     extern __shared__ __align__(1024) unsigned char lds[];
-    const int id = spread(blockIdx.x, gridDim.x);
     Seq sq;
-    if (!find_tile<false>(a, id % tiles, kFewColumns, sq)) return;
-    const int kvh = id / tiles, wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (!find_tile<false>(a, tile_of(a), kFewColumns, sq)) return;
+    const int kvh = head_of(a), wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int64_t columns = int64_t(sq.nq) * a.group, c0 = int64_t(sq.tile) * kFewColumns;
 
     Columns<T, D, CAP, BIAS> col;
@@ -444,10 +441,10 @@ __global__ __launch_bounds__((64 * kFewWaves<T, D>), 1) void k_few(AttnArgs a, i
 
 // Adds the shares up, in order: 16 columns a block, a wave for every fourth.
 template <typename T, int D>
-__global__ __launch_bounds__(256) void k_join(AttnArgs a, int tiles, Shares sh) {
+__global__ __launch_bounds__(256) void k_join(AttnArgs a, Shares sh) {
     Seq sq;
-    if (!find_tile<false>(a, blockIdx.x % tiles, kJoinColumns, sq)) return;
-    const int kvh = blockIdx.x / tiles, lane = threadIdx.x & 63;
+    if (!find_tile<false>(a, tile_of(a), kJoinColumns, sq)) return;
+    const int kvh = head_of(a), lane = threadIdx.x & 63;
     const int64_t columns = int64_t(sq.nq) * a.group;
     for (int c = threadIdx.x >> 6; c < kJoinColumns; c += 4) {
         const int64_t column = int64_t(sq.tile) * kJoinColumns + c;
@@ -519,17 +516,17 @@ hipError_t run(const AttnArgs &a, const Plan &p, hipStream_t s) {
         constexpr int lds = stage > ends ? stage : ends;
         const hipError_t e = max_lds(k_few<T, D, CAP, BIAS>, lds);
         if (e != hipSuccess) return e;
-        k_few<T, D, CAP, BIAS><<<grid, 64 * W, lds, s>>>(a, p.tiles, sh);
+        k_few<T, D, CAP, BIAS><<<grid, 64 * W, lds, s>>>(a, sh);
     } else {
         constexpr int lds = 4 * kTileKeys<T, D> * Tile<T, D>::kRowBytes;
         const hipError_t e = max_lds(k_tiles<T, D, CAP, BIAS>, lds);
         if (e != hipSuccess) return e;
-        k_tiles<T, D, CAP, BIAS><<<grid, 256, lds, s>>>(a, p.tiles, sh);
+        k_tiles<T, D, CAP, BIAS><<<grid, 256, lds, s>>>(a, sh);
     }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && p.splits > 1) {
         const int tiles = int(int64_t(a.q_rows) * a.group / kJoinColumns + a.n_seqs);
-        k_join<T, D><<<uint32_t(tiles) * a.kv_heads, 256, 0, s>>>(a, tiles, sh);
+        k_join<T, D><<<uint32_t(tiles) * a.kv_heads, 256, 0, s>>>(a, sh);
         e = hipGetLastError();
     }
     return e;

@@ -162,24 +162,46 @@ struct Tile {
     }
 };
 
-// A lane's addresses in a tile at LDS address 0, for reads of many tiles: the
-// rest of an address is a constant of the instruction.
-template <int D>
+// Reads operands from tiles at constant LDS addresses: what depends on the lane
+// is computed once, the rest of an address is a constant of the instruction.
+template <typename T, int D>
 struct Lanes {
+    typedef Tile<T, D> L;
+    int lane;
+    uint32_t at;
+    // first: LDS address of tile 0
+    __device__ void init(int l, uint32_t first) {
+        lane = l;
+        at = first;
+    }
+    // Tile::row_frag of row 32 b + lane % 32, and Tile::col_frag
+    __device__ typename Op<T>::Frag row_frag(uint32_t tile, int b, int kk) const {
+        return L::row_frag(at + tile, b * 32 + (lane & 31), kk, lane >> 5);
+    }
+    __device__ typename Op<T>::Frag col_frag(uint32_t tile, int s, int t) const {
+        return L::col_frag(at + tile, s, t, lane);
+    }
+    // To the other of two buffers, `bytes` (a power of two) apart.
+    __device__ void flip(uint32_t bytes) { at ^= bytes; }
+};
+
+template <int D>
+struct Lanes<uint16_t, D> {
     typedef Tile<uint16_t, D> L;
     uint32_t row[D / 16], col[D / 32][2];
-    __device__ void init(int lane) {
+    __device__ void init(int lane, uint32_t first) {
         const uint32_t h = lane >> 5, r = lane & 31, rc = 4 * h + ((lane & 15) >> 2);
 #pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk) row[kk] = opaque(r * L::kRowBytes + (((2 * kk + h) ^ L::turn(r)) << 4));
+        for (int kk = 0; kk < D / 16; ++kk)
+            row[kk] = opaque(first + r * L::kRowBytes + (((2 * kk + h) ^ L::turn(r)) << 4));
 #pragma unroll
         for (int t = 0; t < D / 32; ++t) {
-            const uint32_t c = t * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1), at = rc * L::kRowBytes + (lane & 1) * 8;
+            const uint32_t c = t * 4 + ((lane >> 4) & 1) * 2 + ((lane & 3) >> 1);
+            const uint32_t at = first + rc * L::kRowBytes + (lane & 1) * 8;
             col[t][0] = opaque(at + ((c ^ L::turn(rc)) << 4));
             col[t][1] = opaque(at + 8 * L::kRowBytes + ((c ^ L::turn(rc + 8)) << 4));
         }
     }
-    // Tile::row_frag of row 32 b + lane % 32, and Tile::col_frag
     __device__ bf16x8_t row_frag(uint32_t tile, int b, int kk) const {
         return __builtin_bit_cast(bf16x8_t, *(lds_u32x4 *)(row[kk] + (tile + b * 32 * L::kRowBytes)));
     }
@@ -187,6 +209,12 @@ struct Lanes {
         const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(col[t][0] + (tile + 16 * s * L::kRowBytes)));
         const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4 *)(col[t][1] + (tile + 16 * s * L::kRowBytes)));
         return __builtin_bit_cast(bf16x8_t, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+    __device__ void flip(uint32_t bytes) {
+#pragma unroll
+        for (int kk = 0; kk < D / 16; ++kk) row[kk] ^= bytes;
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t) col[t][0] ^= bytes, col[t][1] ^= bytes;
     }
     // not to be computed again at its uses
     __device__ static uint32_t opaque(uint32_t x) {
@@ -227,19 +255,30 @@ struct Stager {
     typedef Tile<T, D> L;
     static constexpr int kLoads = ROWS * L::kChunks / THREADS;
     static_assert(kLoads >= 1 && ROWS * L::kChunks % THREADS == 0, "whole loads");
-    uint32_t off[kLoads];
+    static constexpr int kPass = THREADS / L::kChunks;  // rows of one load of all threads
+    // Rows 16 apart are stored alike: then one offset serves all loads.
+    static constexpr bool kOne = kPass % 16 == 0;
+    static constexpr uint32_t kBytes = THREADS * 16;  // of one load of all threads
+    uint32_t off[kOne ? 1 : kLoads];
     uint32_t row_bytes, head_bytes;
 
     // thread: 0 .. THREADS - 1
     __device__ void init(int thread, int64_t row_stride, int dim) {
-        row_bytes = uint32_t(row_stride * sizeof(T));
+        row_bytes = __builtin_amdgcn_readfirstlane(uint32_t(row_stride * sizeof(T)));
         head_bytes = uint32_t(dim * sizeof(T));
 #pragma unroll
-        for (int n = 0; n < kLoads; ++n) {
-            const uint32_t id = uint32_t((thread >> 6) * kLoads + n) * 64 + (thread & 63);
-            const uint32_t row = id / L::kChunks, c = (id % L::kChunks) ^ L::turn(row);
+        for (int n = 0; n < (kOne ? 1 : kLoads); ++n) {
+            const uint32_t id = uint32_t(n) * THREADS + thread, row = id / L::kChunks;
+            const uint32_t c = (id % L::kChunks) ^ L::turn(row);
             off[n] = c * 16 < head_bytes ? row * row_bytes + c * 16 : 0x80000000u;
         }
+    }
+    // Of load n.  Offsets of padding stay past every buffer: 2^31 and at most
+    // 96 rows of 2^24 bytes more.
+    __device__ uint32_t offset(int n) const { return kOne ? off[0] + uint32_t(n * kPass) * row_bytes : off[kOne ? 0 : n]; }
+    // The wave's part of a tile.
+    __device__ static uint32_t part(int thread) {
+        return __builtin_amdgcn_readfirstlane(uint32_t(thread >> 6) * 1024u);
     }
     // rows: how many exist from `src` on (wave-uniform, as src and lds)
     __device__ void load(const T *src, int rows, uint32_t lds, int thread) const {
@@ -250,11 +289,11 @@ struct Stager {
         rsrc[1] = __builtin_amdgcn_readfirstlane(uint32_t(p >> 32) & 0xffffu);
         rsrc[2] = __builtin_amdgcn_readfirstlane(len);
         rsrc[3] = 0x00020000u;
-        const uint32_t at = __builtin_amdgcn_readfirstlane(lds + uint32_t(thread >> 6) * (kLoads * 1024));
+        const uint32_t at = __builtin_amdgcn_readfirstlane(lds) + part(thread);
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) {
-            asm volatile("s_mov_b32 m0, %2\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(off[n]), "s"(rsrc),
-                         "s"(at + uint32_t(n) * 1024)
+            asm volatile("s_mov_b32 m0, %2\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset(n)), "s"(rsrc),
+                         "s"(at + uint32_t(n) * kBytes)
                          : "memory", "m0");
         }
     }
@@ -266,9 +305,9 @@ template <typename S, int ROWS>
 struct Walk {
     u32x4_t rsrc;
     uint64_t step;
-    uint32_t at;  // the wave's part of a tile at LDS address 0
+    uint32_t at;  // the wave's part of a tile at the block's first LDS address
     template <typename T>
-    __device__ void init(const S &s, const T *src, int thread) {
+    __device__ void init(const S &s, const T *src, int thread, uint32_t first) {
         const uint64_t p = reinterpret_cast<uint64_t>(src);
         rsrc[0] = __builtin_amdgcn_readfirstlane(uint32_t(p));
         rsrc[1] = __builtin_amdgcn_readfirstlane(uint32_t(p >> 32) & 0xffffu);
@@ -277,15 +316,15 @@ struct Walk {
         const uint64_t bytes = uint64_t(ROWS) * s.row_bytes;
         step = uint64_t(__builtin_amdgcn_readfirstlane(uint32_t(bytes >> 32))) << 32 |
                __builtin_amdgcn_readfirstlane(uint32_t(bytes));
-        at = __builtin_amdgcn_readfirstlane(uint32_t(thread >> 6) * (S::kLoads * 1024));
+        at = __builtin_amdgcn_readfirstlane(first) + S::part(thread);
     }
-    // The next tile, to LDS address TO.
+    // The next tile, to the address TO past the first.
     template <uint32_t TO>
     __device__ void load(const S &s) {
 #pragma unroll
         for (int n = 0; n < S::kLoads; ++n) {
-            asm volatile("s_add_u32 m0, %2, %3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(s.off[n]), "s"(rsrc),
-                         "s"(at), "i"(TO + uint32_t(n) * 1024)
+            asm volatile("s_add_u32 m0, %2, %3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(s.offset(n)), "s"(rsrc),
+                         "s"(at), "i"(TO + uint32_t(n) * S::kBytes)
                          : "memory", "m0", "scc");
         }
         const uint64_t p = (uint64_t(rsrc[1]) << 32 | rsrc[0]) + step;
@@ -549,12 +588,14 @@ struct Score {
     }
 };
 
-// Blocks of one head follow each other on one XCD (block b runs on XCD b % 8),
-// so that its keys and values stay in that XCD's L2.  A bijection of [0, n).
-__device__ inline int spread(int b, int n) {
-    const int per = n / 8, rest = n % 8, x = b % 8, i = b / 8;
-    return x * per + min(x, rest) + i;
-}
+// Block b takes tile b / kv_heads of key head b % kv_heads: the heads' longest
+// tiles start first, and every XCD (block b runs on XCD b % 8) gets tiles of
+// all lengths.  Runs of one head's tiles on one XCD, for its L2, were slower by
+// 11% (16,384 tokens, 6 heads of 64) to 33% (8,192 tokens, causal, 6 heads of
+// 128): the XCDs' shares of a causal batch differ, and a head's keys and values
+// of these sizes are near in the shared cache anyway.
+__device__ inline int tile_of(const AttnArgs &a) { return int(blockIdx.x) / a.kv_heads; }
+__device__ inline int head_of(const AttnArgs &a) { return int(blockIdx.x) % a.kv_heads; }
 
 // The tile width of a head: its channels are padded with zeros to this.
 inline int padded(int dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : 128; }
