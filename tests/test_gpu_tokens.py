@@ -395,6 +395,15 @@ def test_attention_gradient(name, precision):
                            b.contiguous().view(torch.uint8))
 
 
+@pytest.mark.parametrize("precision", PRECISIONS)
+@pytest.mark.parametrize("dim", [32, 64, 128])
+def test_attention_gradient_of_many_sequences(dim, precision):
+    """Enough sequences that a block's waves share its columns and keys in pairs."""
+    seqs = [(i % 41, (7 * i) % 67, i % 9) for i in range(130)]
+    Case(precision, seqs, 4, 4, dim, causal=True, softcap=3.0, bias=True, gap=1).to_gpu().forward().backward() \
+        .check_forward().check_backward()
+
+
 def test_attention_gradient_against_differences():
     """<grad, step> against the difference of the forward pass itself along a
     random step of q, k and v, in float32: the loss sum(dout out) carries
