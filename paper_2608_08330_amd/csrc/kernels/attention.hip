@@ -19,10 +19,10 @@
 // Both take a share of a sequence's keys where whole sequences would leave
 // compute units idle; `join` then adds the shares up in a fixed order.
 //
-// Whole calls, bf16: 16,384 tokens, 6 heads of 64: 526 us (784 TFLOP/s), the
+// Whole calls, bf16: 16,384 tokens, 6 heads of 64: 468 us (881 TFLOP/s), the
 // exponentials beside the products; 8,192 tokens, causal, capped, 6 heads of
-// 128: 195 us; one token against 64 caches of up to 32,768 keys, 2 heads of 128:
-// 181 us (3.3 TB/s).
+// 128: 179 us; one token against 64 caches of up to 32,768 keys, 2 heads of 128:
+// 178 us (3.4 TB/s).
 #include <algorithm>
 #include <type_traits>
 
