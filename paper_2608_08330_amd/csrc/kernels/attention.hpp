@@ -280,7 +280,9 @@ struct Stager {
     __device__ static uint32_t part(int thread) {
         return __builtin_amdgcn_readfirstlane(uint32_t(thread >> 6) * 1024u);
     }
-    // rows: how many exist from `src` on (wave-uniform, as src and lds)
+    // rows: how many exist from `src` on (wave-uniform, as src and lds).  The
+    // s_nop is the wait state that m0 needs before a load reads it; the
+    // compiler adds none inside inline assembly.
     __device__ void load(const T *src, int rows, uint32_t lds, int thread) const {
         const uint64_t p = reinterpret_cast<uint64_t>(src);
         const uint32_t len = rows <= 0 ? 0u : uint32_t(min(rows, ROWS) - 1) * row_bytes + head_bytes;
@@ -292,7 +294,7 @@ struct Stager {
         const uint32_t at = __builtin_amdgcn_readfirstlane(lds) + part(thread);
 #pragma unroll
         for (int n = 0; n < kLoads; ++n) {
-            asm volatile("s_mov_b32 m0, %2\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset(n)), "s"(rsrc),
+            asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset(n)), "s"(rsrc),
                          "s"(at + uint32_t(n) * kBytes)
                          : "memory", "m0");
         }
@@ -318,12 +320,12 @@ struct Walk {
                __builtin_amdgcn_readfirstlane(uint32_t(bytes));
         at = __builtin_amdgcn_readfirstlane(first) + S::part(thread);
     }
-    // The next tile, to the address TO past the first.
+    // The next tile, to the address TO past the first (s_nop: as in Stager).
     template <uint32_t TO>
     __device__ void load(const S &s) {
 #pragma unroll
         for (int n = 0; n < S::kLoads; ++n) {
-            asm volatile("s_add_u32 m0, %2, %3\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(s.offset(n)), "s"(rsrc),
+            asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(s.offset(n)), "s"(rsrc),
                          "s"(at), "i"(TO + uint32_t(n) * S::kBytes)
                          : "memory", "m0", "scc");
         }

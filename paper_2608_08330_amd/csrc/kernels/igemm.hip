@@ -114,11 +114,13 @@ struct Traits<float> {
 // as inline assembly so that the compiler does not treat the DMA as an
 // unknown LDS write that every later LDS read must wait for; the kernel
 // waits for these loads itself with s_waitcnt vmcnt (they retire in issue
-// order, and all of them are drained before the epilogue).
+// order, and all of them are drained before the epilogue).  The s_nop is the
+// wait state that m0 needs before the load reads it; the compiler adds none
+// inside inline assembly.
 __device__ inline void load_lds16(const void *g, uint32_t lds_addr) {
     // the address is wave-uniform (wave index and stage only)
     const uint32_t a = __builtin_amdgcn_readfirstlane(lds_addr);
-    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(g), "s"(a)
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(g), "s"(a)
                  : "memory", "m0");
 }
 

@@ -48,10 +48,12 @@ __device__ inline uint32_t pack_bf16(float a, float b) {
 }
 
 // 16 bytes per lane from global memory into LDS at lds_addr + 16 * lane
-// (lds_addr wave-uniform).  The caller waits with s_waitcnt vmcnt.
+// (lds_addr wave-uniform).  The caller waits with s_waitcnt vmcnt.  The s_nop
+// is the wait state that m0 needs before the load reads it; the compiler adds
+// none inside inline assembly.
 __device__ inline void load_lds16(const void *g, uint32_t lds_addr) {
     const uint32_t a = __builtin_amdgcn_readfirstlane(lds_addr);
-    asm volatile("s_mov_b32 m0, %1\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(g), "s"(a) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(g), "s"(a) : "memory", "m0");
 }
 
 __device__ inline uint32_t lds_address(const void *p) {
