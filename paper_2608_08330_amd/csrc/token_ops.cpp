@@ -125,8 +125,9 @@ Checks check_norm_rope(const rtcc_norm_rope_desc &d, rtcc::kern::NormRopeArgs &a
     copy_stride(a.k_s, d.k_stride, d.rows, d.kv_heads, d.head_dim);
     a.q_weight = d.q_weight;
     a.k_weight = d.k_weight;
-    a.q_weight_stride = d.q_weight_per_head ? d.head_dim : 0;
-    a.k_weight_stride = d.k_weight_per_head ? d.head_dim : 0;
+    // without a weight the flag says nothing: its gradient is one row
+    a.q_weight_stride = d.q_weight && d.q_weight_per_head ? d.head_dim : 0;
+    a.k_weight_stride = d.k_weight && d.k_weight_per_head ? d.head_dim : 0;
     a.positions = d.positions;
     a.inv_freq = d.inv_freq;
     return c;
