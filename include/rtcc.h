@@ -606,7 +606,8 @@ RTCC_API rtcc_status rtcc_norm_rope_grad(const rtcc_norm_rope_grad_desc *desc, v
  * buffers (q_rows, k_rows) and to sequences in ascending order, so that no
  * list, whatever it holds, leads outside them.
  * bf16: the softmax weights are rounded to bf16 for the product with v (their
- * sum is that of the float32 weights). */
+ * sum is that of the float32 weights).  A capped score carries a few roundings
+ * of itself; in bf16 with softcap <= 64 an error of up to softcap * 2^-22. */
 typedef struct rtcc_attn_desc {
     int32_t abi_version;          /* RTCC_ABI_VERSION                                   */
     int32_t precision;            /* rtcc_precision of q, k, v, out                     */

@@ -43,7 +43,7 @@ struct Shares {
 };
 
 // One wave's 32 columns.
-template <typename T, int D, bool CAP, bool BIAS>
+template <typename T, int D, Cap CAP, bool BIAS>
 struct Columns {
     typedef Op<T> M;
     typedef Tile<T, D> L;
@@ -88,13 +88,14 @@ struct Columns {
     // One score from its product; `key` is counted from the half's first key,
     // `away` the query's distance to that.
     __device__ float scored(float x, int key, float away) const {
-        if constexpr (CAP) x = score.capl * score.tanh_of(x);
+        float th;
+        if constexpr (CAP != kNone) x = score.capped<CAP>(x, th);
         else if constexpr (BIAS) x *= score.c1;
         if constexpr (BIAS) x = fmaf(-slope, fabsf(away - float(key)), x);
         return x;
     }
     // What is left to multiply scores by.
-    __device__ float factor() const { return CAP || BIAS ? 1.f : score.c1; }
+    __device__ float factor() const { return CAP != kNone || BIAS ? 1.f : score.c1; }
 
     // Advances the running maximum past `top`, a tile's own in this half.  It
     // follows only where it is left behind by more than 2^8 (any value will do
@@ -198,7 +199,7 @@ constexpr int kTileKeys = sizeof(T) == 2 && D <= 64 ? 64 : 32;
 constexpr int kLeastShare = 128;  // keys
 
 
-template <typename T, int D, bool CAP, bool BIAS>
+template <typename T, int D, Cap CAP, bool BIAS>
 __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_tiles(AttnArgs a, Shares sh) {
     constexpr int N = kTileKeys<T, D>;
     constexpr uint32_t kBytes = N * Tile<T, D>::kRowBytes;
@@ -281,7 +282,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_tiles(AttnArgs 
                 if (e % 2) words[e / 2] = Lanes<T, D>::opaque(__builtin_bit_cast(uint32_t, two));
                 even = w;
             };
-            if constexpr (!CAP && !BIAS) {
+            if constexpr (CAP == kNone && !BIAS) {
 #pragma unroll
                 for (int e = 0; e < E; ++e) raise(e);
                 less = col.advance(top, base);
@@ -294,7 +295,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_tiles(AttnArgs 
                 if (i < H) next[i % NB] = Op<T>::mma(f[i], col.q[i / NB], next[i % NB]);
                 else col.acc[(i - H) % W] = Op<T>::mma(f[i], last[(i - H) / W], col.acc[(i - H) % W]);
                 if (i + kAhead < 2 * H) read(i + kAhead);
-                if constexpr (!CAP && !BIAS) {
+                if constexpr (CAP == kNone && !BIAS) {
 #pragma unroll
                     for (int e = i * E / (2 * H); e < (i + 1) * E / (2 * H); ++e) weigh(e);
                 } else {
@@ -349,7 +350,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_tiles(AttnArgs 
 template <typename T, int D>
 constexpr int kFewWaves = sizeof(T) == 4 && D == 128 ? 2 : 4;
 
-template <typename T, int D, bool CAP, bool BIAS>
+template <typename T, int D, Cap CAP, bool BIAS>
 __global__ __launch_bounds__((64 * kFewWaves<T, D>), 1) void k_few(AttnArgs a, Shares sh) {
     constexpr int W = kFewWaves<T, D>, N = 32;
     constexpr uint32_t kBytes = N * Tile<T, D>::kRowBytes;
@@ -505,7 +506,7 @@ Plan plan_of(const AttnArgs &a) {
     return p;
 }
 
-template <typename T, int D, bool CAP, bool BIAS>
+template <typename T, int D, Cap CAP, bool BIAS>
 hipError_t run(const AttnArgs &a, const Plan &p, hipStream_t s) {
     Shares sh{};
     sh.splits = p.splits;
@@ -539,8 +540,7 @@ hipError_t run(const AttnArgs &a, const Plan &p, hipStream_t s) {
 
 template <typename T, int D>
 hipError_t run(const AttnArgs &a, const Plan &p, hipStream_t s) {
-    if (a.softcap > 0.f) return a.slopes ? run<T, D, true, true>(a, p, s) : run<T, D, true, false>(a, p, s);
-    return a.slopes ? run<T, D, false, true>(a, p, s) : run<T, D, false, false>(a, p, s);
+    return with_terms<T>(a, [&](auto cap, auto bias) { return run<T, D, cap.value, bias.value>(a, p, s); });
 }
 
 template <typename T>

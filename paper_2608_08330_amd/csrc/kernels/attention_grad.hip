@@ -78,7 +78,7 @@ __device__ inline void gather(f32x16_t *acc, float *lds, int group, int turn, in
     }
 }
 
-template <typename T, int D, bool CAP, bool BIAS, int S>
+template <typename T, int D, Cap CAP, bool BIAS, int S>
 __global__ __launch_bounds__(256, (kWavesDq<T, D>)) void k_dq(AttnArgs a, float *stats) {
     typedef Op<T> M;
     typedef Tile<T, D> L;
@@ -138,10 +138,10 @@ __global__ __launch_bounds__(256, (kWavesDq<T, D>)) void k_dq(AttnArgs a, float 
     // P from a product, and the slope of the cap there
     auto weight_of = [&](float x, float away, int j, float &bend) __attribute__((always_inline)) {
         float y;
-        if constexpr (CAP) {
-            const float th = score.tanh_of(x);
+        if constexpr (CAP != kNone) {
+            float th;
+            y = score.capped<CAP>(x, th) - base;
             bend = fmaf(-th, th, 1.f);
-            y = fmaf(score.capl, th, -base);
         } else {
             y = fmaf(x, score.c1, -base);
         }
@@ -165,7 +165,8 @@ __global__ __launch_bounds__(256, (kWavesDq<T, D>)) void k_dq(AttnArgs a, float 
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 const int j = 8 * (r >> 2) + (r & 3);
-                float y = CAP ? score.capl * score.tanh_of(x[r]) : x[r] * score.c1;
+                float y = x[r] * score.c1, th;
+                if constexpr (CAP != kNone) y = score.capped<CAP>(x[r], th);
                 if constexpr (BIAS) y = fmaf(-slope, fabsf(away - float(j)), y);
                 p[r] = j < left ? y : -kInf;
                 top = fmaxf(top, p[r]);
@@ -191,7 +192,7 @@ __global__ __launch_bounds__(256, (kWavesDq<T, D>)) void k_dq(AttnArgs a, float 
             const int j = 8 * (r >> 2) + (r & 3);
             float bend = 1.f;
             float d = weight_of(x[r], away, j, bend) * (dp[r] - delta);
-            if constexpr (CAP) d *= bend;
+            if constexpr (CAP != kNone) d *= bend;
             if (j >= left) d = 0.f;
             ds[r] = d;
         }
@@ -229,7 +230,7 @@ __global__ __launch_bounds__(256, (kWavesDq<T, D>)) void k_dq(AttnArgs a, float 
             if (i == 2 * H - 1) {
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int r = 0; r < 16; ++r) ds[r] *= CAP ? (dp[r] - delta) * x[r] : dp[r] - delta;
+                for (int r = 0; r < 16; ++r) ds[r] *= CAP != kNone ? (dp[r] - delta) * x[r] : dp[r] - delta;
                 w0 = M::pack(ds);
                 w1 = M::pack(ds + 8);
             }
@@ -256,7 +257,7 @@ __global__ __launch_bounds__(256, (kWavesDq<T, D>)) void k_dq(AttnArgs a, float 
     store_column<T, D>(static_cast<T *>(a.dq) + at.row * a.dq_s[0] + at.head * a.dq_s[1], a.dim, h, acc, a.scale);
 }
 
-template <typename T, int D, bool CAP, bool BIAS, int S>
+template <typename T, int D, Cap CAP, bool BIAS, int S>
 __global__ __launch_bounds__(256, (kWavesDkv<T, D>)) void k_dkv(AttnArgs a, const float *row_stats) {
     typedef Op<T> M;
     typedef Tile<T, D> L;
@@ -330,10 +331,10 @@ __global__ __launch_bounds__(256, (kWavesDkv<T, D>)) void k_dkv(AttnArgs a, cons
     auto weight_of = [&](float x, float base, float away, int ir, float slope, float &bend)
         __attribute__((always_inline)) {
         float y;
-        if constexpr (CAP) {
-            const float th = score.tanh_of(x);
+        if constexpr (CAP != kNone) {
+            float th;
+            y = score.capped<CAP>(x, th) - base;
             bend = fmaf(-th, th, 1.f);
-            y = fmaf(score.capl, th, -base);
         } else {
             y = fmaf(x, score.c1, -base);
         }
@@ -360,7 +361,7 @@ __global__ __launch_bounds__(256, (kWavesDkv<T, D>)) void k_dkv(AttnArgs a, cons
             float bend = 1.f;
             p[r] = weight_of(x[r], base[r], away, ir, slope, bend);
             float d = p[r] * (dp[r] - delta[r]);
-            if constexpr (CAP) d *= bend;
+            if constexpr (CAP != kNone) d *= bend;
             if (ir < seen_from) p[r] = d = 0.f;
             ds[r] = d;
         }
@@ -398,7 +399,7 @@ __global__ __launch_bounds__(256, (kWavesDkv<T, D>)) void k_dkv(AttnArgs a, cons
                 if (i >= H && i < 2 * H) {
                     float bend = 1.f;
                     p[r] = weight_of(x[r], base[r], away, 8 * (r >> 2) + (r & 3), slope, bend);
-                    if constexpr (CAP) x[r] = bend * p[r];
+                    if constexpr (CAP != kNone) x[r] = bend * p[r];
                     else x[r] = p[r];
                 } else if (i >= 2 * H && i < 3 * H) {
                     x[r] *= dp[r] - delta[r];
@@ -446,7 +447,7 @@ template <typename T, int D, int S>
 constexpr int kLds = std::max(4 * kRows<S> * Tile<T, D>::kRowBytes + 4 * kRows<S> * 4,
                               (4 / S) * (S - 1) * 32 * (D + 4) * 4);
 
-template <typename T, int D, bool CAP, bool BIAS, int S>
+template <typename T, int D, Cap CAP, bool BIAS, int S>
 hipError_t run_dq(const AttnArgs &a, hipStream_t s) {
     const int tiles = int(int64_t(a.q_rows) * a.group / (kSide / S) + a.n_seqs);
     const hipError_t e = max_lds(k_dq<T, D, CAP, BIAS, S>, kLds<T, D, S>);
@@ -454,7 +455,7 @@ hipError_t run_dq(const AttnArgs &a, hipStream_t s) {
     k_dq<T, D, CAP, BIAS, S><<<uint32_t(tiles) * a.kv_heads, 256, kLds<T, D, S>, s>>>(a, static_cast<float *>(a.workspace));
     return hipGetLastError();
 }
-template <typename T, int D, bool CAP, bool BIAS, int S>
+template <typename T, int D, Cap CAP, bool BIAS, int S>
 hipError_t run_dkv(const AttnArgs &a, hipStream_t s) {
     const int tiles = a.k_rows / (kSide / S) + a.n_seqs;
     const hipError_t e = max_lds(k_dkv<T, D, CAP, BIAS, S>, kLds<T, D, S>);
@@ -465,7 +466,7 @@ hipError_t run_dkv(const AttnArgs &a, hipStream_t s) {
 }
 
 // workspace: lse in log 2 units and delta of every row, [2][q_heads][q_rows]
-template <typename T, int D, bool CAP, bool BIAS>
+template <typename T, int D, Cap CAP, bool BIAS>
 hipError_t run(const AttnArgs &a, hipStream_t s) {
     constexpr int kMost = sizeof(T) == 4 && D == 128 ? 2 : 4;  // as the LDS holds
     const int wanted = 4 * compute_units();
@@ -482,8 +483,7 @@ hipError_t run(const AttnArgs &a, hipStream_t s) {
 
 template <typename T, int D>
 hipError_t run(const AttnArgs &a, hipStream_t s) {
-    if (a.softcap > 0.f) return a.slopes ? run<T, D, true, true>(a, s) : run<T, D, true, false>(a, s);
-    return a.slopes ? run<T, D, false, true>(a, s) : run<T, D, false, false>(a, s);
+    return with_terms<T>(a, [&](auto cap, auto bias) { return run<T, D, cap.value, bias.value>(a, s); });
 }
 
 template <typename T>

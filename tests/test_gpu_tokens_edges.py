@@ -38,3 +38,38 @@ def test_gradient_of_an_absent_weight_is_one_row(precision):
         size = (np.linalg.norm(_f64(c.dy[i]), axis=-1, keepdims=True) * np.abs(x) /
                 np.sqrt((x * x).mean(-1, keepdims=True) + c.eps)).sum((0, 1))
         assert (np.abs(_f64(dw[i][0]) - want) <= (dim + 64 + 2 * np.sqrt(rows * heads[i])) * U * size).all()
+
+
+class Capped(Case):
+    """A case whose allowed error of a score follows the score, not the cap:
+    the product's dim + 8 roundings and 8 more of the tanh.  bf16 with caps up
+    to 64 has the header's 2^-22 of the cap instead."""
+
+    def errors(self):
+        cap, self.softcap = self.softcap, 0.0
+        s, _p = super().errors()
+        self.softcap = cap
+        q, k = np.abs(_f64(self.q)), np.abs(_f64(self.k))
+        g = q.shape[1] // k.shape[1]
+        most = max((q[q0:q0 + nq, h] @ k[k0:k0 + nk, h // g].T).max() for q0, nq, k0, nk, _p in self.seqs
+                   for h in range(q.shape[1]))
+        s += cap * 2.0 ** -22 if self.precision == "bf16" and cap <= 64 else 8 * U * self.scale * most
+        return s, 2 * s + max(nk for _a, _b, _c, nk, _p in self.seqs) * U + 2.0 ** -20
+
+
+@pytest.mark.parametrize("precision", PRECISIONS)
+@pytest.mark.parametrize("dim,bias,causal", [(64, False, False), (32, True, True), (128, True, False)])
+@pytest.mark.parametrize("cap", [2.0 ** -130, 1e-3, 2.5, 50.0, 64.0, 100.0, 1e4, 1e6, 1e8, 3e38])
+def test_caps_of_every_size(cap, dim, bias, causal, precision):
+    c = Capped(precision, [(150, 150, 0), (33, 200, 0)], 4, 2, dim, causal=causal, bias=bias,
+               softcap=float(np.float32(cap)))
+    o = c.oracle()
+    c.to_gpu().forward().check_forward(o).backward().check_backward(o)
+
+
+@pytest.mark.parametrize("precision", PRECISIONS)
+@pytest.mark.parametrize("cap", [50.0, 1e6])
+def test_caps_for_single_tokens(cap, precision):
+    """The kernel for few queries."""
+    c = Capped(precision, [(1, 300, 0), (2, 90, 0), (1, 1, 0)], 4, 1, 64, causal=True, softcap=cap)
+    c.to_gpu().forward().check_forward()
