@@ -636,9 +636,10 @@ RTCC_API rtcc_status rtcc_attention(const rtcc_attn_desc *desc, void *workspace,
                                     void *hip_stream);
 
 /* Gradients of rtcc_attention with respect to q, k and v.  fwd describes the
- * forward call whose out and lse (required) are read.  dout: as out.  dq, dk,
- * dv: as q, k, v; written, not added to; dk and dv sum over the query heads of
- * a key head, in a fixed order (the results of two calls are the same bits).
+ * forward call whose out and lse (required) are read; k_rows * kv_heads is
+ * below 2^35.  dout: as out.  dq, dk, dv: as q, k, v; written, not added to; dk
+ * and dv sum over the query heads of a key head, in a fixed order (the results
+ * of two calls are the same bits).
  * Key ranges of different sequences must not overlap (their sums would race:
  * undefined values).  Rows of q, k, v in no sequence are not written; a key
  * that no query sees gets 0.  bf16: the softmax weights and their gradients

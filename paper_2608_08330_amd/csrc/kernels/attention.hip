@@ -489,19 +489,18 @@ __global__ __launch_bounds__(256) void k_join(AttnArgs a, Shares sh) {
 
 struct Plan {
     bool few;
-    int tiles, splits;
+    int64_t blocks;
+    int splits;
 };
 
 Plan plan_of(const AttnArgs &a) {
     Plan p;
     const int64_t columns = int64_t(a.q_rows) * a.group;
     p.few = columns <= int64_t(kFewColumns) * a.n_seqs;
-    const int per = p.few ? kFewColumns : kTileColumns;
-    p.tiles = int(columns / per + a.n_seqs);  // at least the sum over sequences of their rounded tiles
-    const int64_t blocks = int64_t(p.tiles) * a.kv_heads;
+    p.blocks = column_blocks(a, p.few ? kFewColumns : kTileColumns);
     const int64_t wanted = int64_t(compute_units()) * (p.few ? 4 : 2);
     const int64_t keys = (a.k_rows + a.n_seqs - 1) / std::max(a.n_seqs, 1);
-    int64_t s = std::min<int64_t>((wanted + blocks - 1) / blocks, (keys + 255) / 256);
+    int64_t s = std::min<int64_t>((wanted + p.blocks - 1) / p.blocks, (keys + 255) / 256);
     p.splits = int(std::max<int64_t>(1, std::min<int64_t>(s, 64)));
     return p;
 }
@@ -515,9 +514,10 @@ hipError_t run(const AttnArgs &a, const Plan &p, hipStream_t s) {
         sh.o = static_cast<float *>(a.workspace);
         sh.ml = reinterpret_cast<float2 *>(sh.o + rows * D);
     }
-    const dim3 grid(uint32_t(p.tiles) * a.kv_heads, p.splits);
+    constexpr int W = kFewWaves<T, D>;
+    const Fold f = fold(p.blocks, p.few ? 64 * W : 256);
+    const dim3 grid(f.x, p.splits, f.z);
     if (p.few) {
-        constexpr int W = kFewWaves<T, D>;
         constexpr int stage = W * 4 * 32 * Tile<T, D>::kRowBytes, ends = W * 32 * (8 + (D + 4) * 4);
         constexpr int lds = stage > ends ? stage : ends;
         const hipError_t e = max_lds(k_few<T, D, CAP, BIAS>, lds);
@@ -531,8 +531,8 @@ hipError_t run(const AttnArgs &a, const Plan &p, hipStream_t s) {
     }
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && p.splits > 1) {
-        const int tiles = int(int64_t(a.q_rows) * a.group / kJoinColumns + a.n_seqs);
-        k_join<T, D><<<uint32_t(tiles) * a.kv_heads, 256, 0, s>>>(a, sh);
+        const Fold j = fold(column_blocks(a, kJoinColumns), 256);
+        k_join<T, D><<<dim3(j.x, 1, j.z), 256, 0, s>>>(a, sh);
         e = hipGetLastError();
     }
     return e;

@@ -376,33 +376,34 @@ __device__ inline int uniform(int x) { return __builtin_amdgcn_readfirstlane(x);
 // Sequence and tile within it of tile `t` of the batch, a tile being `per`
 // units: columns (queries x heads of a group) with KEYS = false, keys with
 // KEYS = true.  False past the last tile.  Every wave of a block gets the same
-// answer, in scalar registers.
+// answer, in scalar registers.  Sums of 64 sequences' tiles (of at least 64
+// units where there are many) reach 2^31 at most, where lists overlap.
 template <bool KEYS>
-__device__ inline bool find_tile(const AttnArgs &a, int t, int per, Seq &q) {
+__device__ inline bool find_tile(const AttnArgs &a, int tile, int per, Seq &q) {
     const int lane = threadIdx.x & 63;
-    int before = 0;  // tiles of the sequences looked at
+    uint32_t t = tile;  // less the tiles of the sequences looked at
     for (int s0 = 0; s0 < a.n_seqs; s0 += 64) {
         const int s = s0 + lane;
-        int n = 0;
+        uint32_t n = 0;
         if (s < a.n_seqs) {
             int from, len;
             if constexpr (KEYS) k_range(a, s, from, len);
             else q_range(a, s, from, len);
             const int64_t units = KEYS ? len : int64_t(len) * a.group;
-            n = int((units + per - 1) / per);
+            n = uint32_t((units + per - 1) / per);
         }
-        int sum = n;  // inclusive over the lanes
+        uint32_t sum = n;  // inclusive over the lanes
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
-            const int up = __shfl_up(sum, d);
+            const uint32_t up = __shfl_up(sum, d);
             if (lane >= d) sum += up;
         }
-        const int total = __builtin_amdgcn_readlane(sum, 63);
-        if (t - before < total) {
-            const unsigned long long past = __ballot(sum > t - before);
+        const uint32_t total = __builtin_amdgcn_readlane(sum, 63);
+        if (t < total) {
+            const unsigned long long past = __ballot(sum > t);
             const int at = __builtin_ctzll(past);
             q.s = s0 + at;
-            q.tile = t - before - (at ? __builtin_amdgcn_readlane(sum, at - 1) : 0);
+            q.tile = int(t - (at ? uint32_t(__builtin_amdgcn_readlane(sum, at - 1)) : 0u));
             q.s = uniform(q.s);
             q.tile = uniform(q.tile);
             q_range(a, q.s, q.q0, q.nq);
@@ -415,7 +416,7 @@ __device__ inline bool find_tile(const AttnArgs &a, int t, int per, Seq &q) {
             q.prefix = uniform(q.prefix);
             return true;
         }
-        before += total;
+        t -= total;
     }
     return false;
 }
@@ -618,14 +619,15 @@ struct Score {
     }
 };
 
-// Block b takes tile b / kv_heads of key head b % kv_heads: the heads' longest
+// Block b (counted over x and z, see fold) takes tile b / kv_heads of key head b % kv_heads: the heads' longest
 // tiles start first, and every XCD (block b runs on XCD b % 8) gets tiles of
 // all lengths.  Runs of one head's tiles on one XCD, for its L2, were slower by
 // 11% (16,384 tokens, 6 heads of 64) to 33% (8,192 tokens, causal, 6 heads of
 // 128): the XCDs' shares of a causal batch differ, and a head's keys and values
 // of these sizes are near in the shared cache anyway.
-__device__ inline int tile_of(const AttnArgs &a) { return int(blockIdx.x) / a.kv_heads; }
-__device__ inline int head_of(const AttnArgs &a) { return int(blockIdx.x) % a.kv_heads; }
+__device__ inline int block() { return int(blockIdx.z * gridDim.x + blockIdx.x); }
+__device__ inline int tile_of(const AttnArgs &a) { return block() / a.kv_heads; }
+__device__ inline int head_of(const AttnArgs &a) { return block() % a.kv_heads; }
 
 // The tile width of a head: its channels are padded with zeros to this.
 inline int padded(int dim) { return dim <= 32 ? 32 : dim <= 64 ? 64 : 128; }

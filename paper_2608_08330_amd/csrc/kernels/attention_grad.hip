@@ -449,18 +449,18 @@ constexpr int kLds = std::max(4 * kRows<S> * Tile<T, D>::kRowBytes + 4 * kRows<S
 
 template <typename T, int D, Cap CAP, bool BIAS, int S>
 hipError_t run_dq(const AttnArgs &a, hipStream_t s) {
-    const int tiles = int(int64_t(a.q_rows) * a.group / (kSide / S) + a.n_seqs);
+    const Fold f = fold(column_blocks(a, kSide / S), 256);
     const hipError_t e = max_lds(k_dq<T, D, CAP, BIAS, S>, kLds<T, D, S>);
     if (e != hipSuccess) return e;
-    k_dq<T, D, CAP, BIAS, S><<<uint32_t(tiles) * a.kv_heads, 256, kLds<T, D, S>, s>>>(a, static_cast<float *>(a.workspace));
+    k_dq<T, D, CAP, BIAS, S><<<dim3(f.x, 1, f.z), 256, kLds<T, D, S>, s>>>(a, static_cast<float *>(a.workspace));
     return hipGetLastError();
 }
 template <typename T, int D, Cap CAP, bool BIAS, int S>
 hipError_t run_dkv(const AttnArgs &a, hipStream_t s) {
-    const int tiles = a.k_rows / (kSide / S) + a.n_seqs;
+    const Fold f = fold(key_blocks(a, kSide / S), 256);
     const hipError_t e = max_lds(k_dkv<T, D, CAP, BIAS, S>, kLds<T, D, S>);
     if (e != hipSuccess) return e;
-    k_dkv<T, D, CAP, BIAS, S><<<uint32_t(tiles) * a.kv_heads, 256, kLds<T, D, S>, s>>>(
+    k_dkv<T, D, CAP, BIAS, S><<<dim3(f.x, 1, f.z), 256, kLds<T, D, S>, s>>>(
         a, static_cast<const float *>(a.workspace));
     return hipGetLastError();
 }

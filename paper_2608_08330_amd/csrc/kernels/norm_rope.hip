@@ -107,8 +107,9 @@ struct Chunk {
 
 template <typename T, int G, bool IL>
 __global__ __launch_bounds__(256) void k_norm_rope(NormRopeArgs a, int per) {
-    const int row = int(blockIdx.x * (256u / G) + threadIdx.x / G);
-    if (row >= a.rows) return;
+    const uint32_t place = (blockIdx.z * gridDim.x + blockIdx.x) * (256u / G) + threadIdx.x / G;
+    if (place >= uint32_t(a.rows)) return;
+    const int row = int(place);
     const Lane<IL> lane(threadIdx.x % G, a.dim);
     const Chunk c(a, per, blockIdx.y);
     int64_t out_row = row;
@@ -286,7 +287,7 @@ int group_of(int dim) { return dim <= 16 ? 1 : dim <= 32 ? 2 : dim <= 64 ? 4 : 8
 // units without eight waves each.
 Cut forward_cut(const NormRopeArgs &a) {
     Cut c;
-    c.blocks = ceil_div(a.rows, 256 / group_of(a.dim));
+    c.blocks = int(row_tiles(a.rows, 256 / group_of(a.dim)));
     c.per = std::max(std::max(a.q_heads, a.kv_heads), 1);
     auto chunks = [&](int per) {
         return ceil_div(a.q_heads, per) + ceil_div(a.kv_heads, per) * (a.v ? 2 : 1);
@@ -299,7 +300,7 @@ Cut forward_cut(const NormRopeArgs &a) {
 Cut gradient_cut(const NormRopeArgs &a) {
     Cut c;
     const bool per_head = (a.dq_weight && a.q_weight_stride) || (a.dk_weight && a.k_weight_stride);
-    c.blocks = ceil_div(a.rows, 256 / group_of(a.dim));
+    c.blocks = int(row_tiles(a.rows, 256 / group_of(a.dim)));
     c.per = per_head ? 1 : std::max(std::max(a.q_heads, a.kv_heads), 1);
     auto chunks = [&](int per) { return ceil_div(a.q_heads, per) + ceil_div(a.kv_heads, per); };
     while (c.per > 1 && int64_t(c.blocks) * chunks(c.per) < 2 * compute_units()) c.per = (c.per + 1) / 2;
@@ -311,7 +312,8 @@ Cut gradient_cut(const NormRopeArgs &a) {
 
 template <typename T, int G>
 hipError_t run(const NormRopeArgs &a, bool grad, const Cut &c, hipStream_t s) {
-    const dim3 grid(c.blocks, c.chunks);
+    const Fold f = fold(c.blocks, 256);  // the gradient's blocks are few
+    const dim3 grid(f.x, c.chunks, f.z);
     if (grad) {
         if (a.interleaved) k_norm_rope_grad<T, G, true><<<grid, 256, 0, s>>>(a, c.per);
         else k_norm_rope_grad<T, G, false><<<grid, 256, 0, s>>>(a, c.per);

@@ -5,6 +5,7 @@
 // has validated the descriptor.  Return value: a hipError_t as int.
 #pragma once
 
+#include <algorithm>
 #include <cstddef>
 #include <cstdint>
 
@@ -47,6 +48,29 @@ struct AttnArgs {
     int64_t do_s[2], dq_s[2], dk_s[2], dv_s[2];
     void *workspace;
 };
+
+// Blocks of a launch, of which a kernel counts blockIdx.z * gridDim.x +
+// blockIdx.x: HIP takes fewer than 2^32 threads an axis.  The description's
+// limits keep every number of blocks below 2^31.
+struct Fold {
+    uint32_t x, z;
+};
+inline Fold fold(int64_t blocks, int threads) {
+    const int64_t most = ((int64_t(1) << 32) - 1) / threads, z = std::max<int64_t>(1, (blocks + most - 1) / most);
+    return {uint32_t((blocks + z - 1) / z), uint32_t(z)};
+}
+// Tiles of `per` rows.
+inline int64_t row_tiles(int64_t rows, int per) { return (rows + per - 1) / per; }
+// Tiles of `per` columns (queries x heads of a group) or keys, for all key
+// heads: at least the sum over the sequences of their rounded tiles.
+inline int64_t column_blocks(const AttnArgs &a, int per) {
+    return (int64_t(a.q_rows) * a.group / per + a.n_seqs) * a.kv_heads;
+}
+inline int64_t key_blocks(const AttnArgs &a, int per) {
+    return (int64_t(a.k_rows) / per + a.n_seqs) * a.kv_heads;
+}
+// Of the gradient's smallest tiles of a long batch (64 keys): 2^29 + 2^26 blocks.
+constexpr int64_t kMaxGradKeys = int64_t(1) << 35;  // k_rows * kv_heads
 
 size_t norm_rope_grad_workspace(const NormRopeArgs &a);
 int norm_rope(const NormRopeArgs &a, void *stream);

@@ -214,6 +214,7 @@ Checks check_attention_grad(const rtcc_attn_grad_desc &d, rtcc::kern::AttnArgs &
     if (f.n_seqs > 0) {
         const int32_t elem = f.precision == RTCC_PREC_BF16 ? 2 : 4;
         c.need(f.lse || f.q_rows == 0, "lse is NULL");
+        c.need(f.k_rows * f.kv_heads < rtcc::kern::kMaxGradKeys, "k_rows * kv_heads out of range");
         c.tensor(d.dout, d.dout_stride, f.q_rows, f.q_heads, f.head_dim, elem, "dout");
         c.tensor(d.dq, d.dq_stride, f.q_rows, f.q_heads, f.head_dim, elem, "dq");
         c.tensor(d.dk, d.dk_stride, f.k_rows, f.kv_heads, f.head_dim, elem, "dk");

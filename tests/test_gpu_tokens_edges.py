@@ -73,3 +73,30 @@ def test_caps_for_single_tokens(cap, precision):
     """The kernel for few queries."""
     c = Capped(precision, [(1, 300, 0), (2, 90, 0), (1, 1, 0)], 4, 1, 64, causal=True, softcap=cap)
     c.to_gpu().forward().check_forward()
+
+
+def test_more_blocks_than_one_axis_holds():
+    """16,400 sequences of one token with 1,024 heads: 17.3 M blocks.  A token
+    that sees itself alone returns its value and its output's gradient, and has
+    no gradient of its score."""
+    import torch
+    n, heads, dim = 16400, 1024, 16
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    q, k, v, do = (torch.randn(n, heads, dim, generator=gen, device="cuda", dtype=torch.bfloat16) for _ in range(4))
+    out, dq, dk, dv = (torch.full_like(q, float("nan")) for _ in range(4))
+    lse = torch.empty(heads, n, device="cuda")
+    offsets = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    d = R.attention_desc(q, k, v, out, offsets, offsets, lse=lse)
+    assert R.rtcc_attention_workspace(d) == 0
+    R.rtcc_attention(d, 0, 0)
+    torch.cuda.synchronize()
+    assert torch.equal(out, v)
+    g = R.attention_grad_desc(d, do, dq, dk, dv)
+    m = R.rtcc_attention_grad_workspace(g)
+    space = _workspace(m)
+    R.rtcc_attention_grad(g, space.data_ptr(), m)
+    torch.cuda.synchronize()
+    assert torch.equal(dv, do)
+    # two orders of a product of 16 terms, each at most 6^2 in size, and a weight's 2^-20
+    worst = ((2 * 16 + 8) * U * 16 + 2.0 ** -20) * 36 * 6 * dim ** -0.5
+    assert dq.abs().max().item() <= worst and dk.abs().max().item() <= worst
