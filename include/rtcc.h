@@ -560,7 +560,7 @@ typedef struct rtcc_norm_rope_desc {
     void *q_out, *k_out, *v_out;
     int64_t q_stride[2], k_stride[2], v_stride[2];
     int64_t q_out_stride[2], k_out_stride[2], v_out_stride[2];
-    const float *q_weight, *k_weight; /* [head_dim], or [heads][head_dim]; NULL: all 1  */
+    const float *q_weight, *k_weight; /* [head_dim], or [heads][head_dim], at any float's address; NULL: all 1 */
     int32_t q_weight_per_head, k_weight_per_head; /* 0: one weight for all heads; no matter where the weight is NULL */
     const float *positions;       /* [rows][n_axes], contiguous                         */
     const float *inv_freq;        /* [sum of sections]                                  */

@@ -39,6 +39,13 @@ __device__ inline void load8(const float *p, float *v) {
     v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
     v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
 }
+// of a weight: float32 at any address of a float
+__device__ inline void load8_weight(const float *p, float *v) {
+    typedef float f32x4_t __attribute__((ext_vector_type(4), aligned(4)));
+    const f32x4_t a = reinterpret_cast<const f32x4_t *>(p)[0], b = reinterpret_cast<const f32x4_t *>(p)[1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = a[e], v[e + 4] = b[e];
+}
 __device__ inline void store8(uint16_t *p, const float *v) {
     typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
     bf16x8_t f;
@@ -149,8 +156,8 @@ __global__ __launch_bounds__(256) void k_norm_rope(NormRopeArgs a, int per) {
         const float r = rsqrtf(group_sum<G>(ss) / float(a.dim) + a.eps);
         if (!lane.on) continue;
         if (weight) {
-            load8(weight + h * wh + lane.lo, w);
-            load8(weight + h * wh + lane.hi, w + 8);
+            load8_weight(weight + h * wh + lane.lo, w);
+            load8_weight(weight + h * wh + lane.hi, w + 8);
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) u[e] *= weight ? r * w[e] : r;
@@ -193,8 +200,8 @@ __global__ __launch_bounds__(256) void k_norm_rope_grad(NormRopeArgs a, int per)
                 load8(dy + h * gh + lane.lo, g);
                 load8(dy + h * gh + lane.hi, g + 8);
                 if (weight) {
-                    load8(weight + h * wh + lane.lo, w);
-                    load8(weight + h * wh + lane.hi, w + 8);
+                    load8_weight(weight + h * wh + lane.lo, w);
+                    load8_weight(weight + h * wh + lane.hi, w + 8);
                 }
             }
             float ss = 0.f;

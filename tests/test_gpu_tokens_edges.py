@@ -100,3 +100,35 @@ def test_more_blocks_than_one_axis_holds():
     # two orders of a product of 16 terms, each at most 6^2 in size, and a weight's 2^-20
     worst = ((2 * 16 + 8) * U * 16 + 2.0 ** -20) * 36 * 6 * dim ** -0.5
     assert dq.abs().max().item() <= worst and dk.abs().max().item() <= worst
+
+
+@pytest.mark.parametrize("precision", PRECISIONS)
+@pytest.mark.parametrize("weights", ["shared", "per_head"])
+@pytest.mark.parametrize("shift", [1, 2, 3])
+def test_weights_inside_a_larger_buffer(shift, weights, precision):
+    """Weights and their gradients at 4-byte aligned addresses: the same bits as
+    at aligned ones."""
+    import torch
+    rows, heads, dim = 70, (3, 2), 80
+    c = Rope(precision, rows, *heads, dim, (10, 10, 10), True, weights=weights)
+    dy = [g.cuda() for g in c.dy]
+
+    def run(shift):
+        def inside(w):
+            buffer = torch.full((w.numel() + 8,), float("nan"), device="cuda")
+            at = buffer[shift:shift + w.numel()].view(w.shape)
+            return at.copy_(w)
+        c.gw = [inside(w) for w in c.w]
+        out = [torch.empty_like(g) for g in dy]
+        d = c.desc(out)
+        R.rtcc_norm_rope(d)
+        dx, dw = [torch.empty_like(g) for g in dy], [inside(torch.zeros_like(w)) for w in c.w]
+        g = R.norm_rope_grad_desc(d, dy[0], dy[1], dx[0], dx[1], dw[0], dw[1])
+        n = R.rtcc_norm_rope_grad_workspace(g)
+        space = _workspace(n)
+        R.rtcc_norm_rope_grad(g, space.data_ptr(), n)
+        torch.cuda.synchronize()
+        return out + dx + dw
+
+    for a, b in zip(run(0), run(shift)):
+        assert torch.equal(a, b)
