@@ -603,9 +603,9 @@ def rtcc_rotated_nms_noalloc(device_records, n, max_candidates, iou_threshold, d
 # token operators
 # ----------------------------------------------------------------------------
 # The *_desc functions describe tensors (torch tensors, or anything with their
-# data_ptr(), stride(), shape and dtype): [rows, heads, head_dim], any row and
-# head strides the library takes.  A description holds addresses only; the
-# caller keeps the tensors.  The rtcc_* functions take a description, a
+# data_ptr(), get_device(), stride(), shape and dtype): [rows, heads, head_dim],
+# any row and head strides the library takes, all on one device.  A description
+# holds addresses only; the caller keeps the tensors.  The rtcc_* functions take a description, a
 # workspace address of the size their *_workspace function names, and a HIP
 # stream handle (integer, 0 = the null stream), and return once the work is
 # enqueued.
@@ -613,18 +613,42 @@ def rtcc_rotated_nms_noalloc(device_records, n, max_candidates, iou_threshold, d
 _PRECISION = {"torch.float32": RTCC_PREC_FP32, "torch.bfloat16": RTCC_PREC_BF16}
 
 
+def _place(d, name, x):
+    """Fill the pointer of tensor `name` of description d, whose tensors are all
+    on one device; -1 is host memory, which only the host test library takes."""
+    device = x.get_device()
+    if getattr(d, "device", device) != device:
+        raise ValueError("%s is on another device than the tensors before it" % name)
+    d.device = device
+    setattr(d, name, x.data_ptr())
+
+
+def _on_gpu(d, kind):
+    if kind == "gpu" and getattr(d, "device", 0) < 0:
+        raise ValueError("the description's tensors are in host memory")
+
+
+def _grad_of(cls, fwd):
+    g = cls(fwd=fwd)
+    if hasattr(fwd, "device"):
+        g.device = fwd.device
+    return g
+
+
 def _tokens(d, name, x, like=None):
     """Fill the pointer and strides of tensor `name` of description d.
     like: (shape, dtype) it has to have; None entries are free."""
-    if x.ndim != 3 or (x.shape[2] > 1 and x.stride(2) != 1):
+    s = x.stride()
+    if len(s) != 3 or (s[2] != 1 and x.shape[2] > 1):
         raise ValueError("%s must be [rows, heads, head_dim] with contiguous heads" % name)
     if like is not None:
-        if x.dtype != like[1]:
-            raise ValueError("%s must have dtype %s" % (name, like[1]))
-        if any(w is not None and w != g for w, g in zip(like[0], x.shape)):
-            raise ValueError("%s must have shape %s" % (name, tuple(like[0])))
-    s = x.stride()
-    setattr(d, name, x.data_ptr())
+        shape, dtype = like
+        if x.dtype != dtype:
+            raise ValueError("%s must have dtype %s" % (name, dtype))
+        rows, heads, dim = x.shape
+        if shape[0] not in (None, rows) or shape[1] not in (None, heads) or shape[2] not in (None, dim):
+            raise ValueError("%s must have shape %s" % (name, tuple(shape)))
+    _place(d, name, x)
     a = getattr(d, name + "_stride")
     a[0], a[1] = s[0], s[1]
 
@@ -633,7 +657,7 @@ def _flat(d, name, x, shape, dtype):
     """Fill the pointer of a contiguous tensor of the given shape and dtype."""
     if tuple(x.shape) != tuple(shape) or str(x.dtype) != dtype or not x.is_contiguous():
         raise ValueError("%s must be a contiguous %s tensor of shape %s" % (name, dtype, tuple(shape)))
-    setattr(d, name, x.data_ptr())
+    _place(d, name, x)
 
 
 def _precision_of(x):
@@ -689,7 +713,7 @@ def norm_rope_desc(q, k, q_out, k_out, q_weight, k_weight, positions, inv_freq, 
 def norm_rope_grad_desc(fwd, dq_out, dk_out, dq, dk, dq_weight=None, dk_weight=None):
     """Description of the gradients of the call that fwd (norm_rope_desc)
     describes; dq_weight and dk_weight: float32 of the weights' shapes."""
-    g = rtcc_norm_rope_grad_desc(fwd=fwd)
+    g = _grad_of(rtcc_norm_rope_grad_desc, fwd)
     dtype = None
     for names, heads in ((("dq_out", "dq"), fwd.q_heads), (("dk_out", "dk"), fwd.kv_heads)):
         for name in names:
@@ -741,7 +765,7 @@ def attention_desc(q, k, v, out, q_offsets, k_offsets, k_lens=None, prefix_lens=
 def attention_grad_desc(fwd, dout, dq, dk, dv):
     """Description of the gradients of the call that fwd (attention_desc, with
     its lse) describes."""
-    g = rtcc_attn_grad_desc(fwd=fwd)
+    g = _grad_of(rtcc_attn_grad_desc, fwd)
     if _precision_of(dout) != fwd.precision:
         raise ValueError("dout must have the forward tensors' dtype")
     for name, x, rows, heads in (("dout", dout, fwd.q_rows, fwd.q_heads), ("dq", dq, fwd.q_rows, fwd.q_heads),
@@ -759,6 +783,7 @@ def _workspace_call(fn, desc, kind):
 
 def rtcc_norm_rope(desc, stream=0, kind="gpu"):
     """Norm and rotation of queries and keys (norm_rope_desc)."""
+    _on_gpu(desc, kind)
     lib = load(kind)
     _free_call(lib, lib.rtcc_norm_rope(ctypes.byref(desc), _P(stream)))
 
@@ -769,6 +794,7 @@ def rtcc_norm_rope_grad_workspace(desc, kind="gpu"):
 
 def rtcc_norm_rope_grad(desc, workspace, workspace_bytes, stream=0, kind="gpu"):
     """Gradients of rtcc_norm_rope (norm_rope_grad_desc)."""
+    _on_gpu(desc, kind)
     lib = load(kind)
     _free_call(lib, lib.rtcc_norm_rope_grad(ctypes.byref(desc), _P(workspace), workspace_bytes, _P(stream)))
 
@@ -779,6 +805,7 @@ def rtcc_attention_workspace(desc, kind="gpu"):
 
 def rtcc_attention(desc, workspace, workspace_bytes, stream=0, kind="gpu"):
     """Attention of packed sequences (attention_desc)."""
+    _on_gpu(desc, kind)
     lib = load(kind)
     _free_call(lib, lib.rtcc_attention(ctypes.byref(desc), _P(workspace), workspace_bytes, _P(stream)))
 
@@ -789,6 +816,7 @@ def rtcc_attention_grad_workspace(desc, kind="gpu"):
 
 def rtcc_attention_grad(desc, workspace, workspace_bytes, stream=0, kind="gpu"):
     """Gradients of rtcc_attention (attention_grad_desc)."""
+    _on_gpu(desc, kind)
     lib = load(kind)
     _free_call(lib, lib.rtcc_attention_grad(ctypes.byref(desc), _P(workspace), workspace_bytes, _P(stream)))
 
