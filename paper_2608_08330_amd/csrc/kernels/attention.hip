@@ -51,7 +51,8 @@ struct Columns {
     f32x16_t acc[D / 32];
     float m, l;
     int lane, h, limit, first_limit, last_limit;
-    float place, slope;
+    int place;  // of the query; distances are taken in whole numbers
+    float slope;
     Column at;
     Score score;
 
@@ -63,7 +64,7 @@ struct Columns {
         limit = limit_of(a, sq, at.i);
         first_limit = __builtin_amdgcn_readlane(limit, 0);
         last_limit = __builtin_amdgcn_readlane(limit, 31);
-        place = float(sq.nk - sq.nq + at.i);
+        place = sq.nk - sq.nq + at.i;
         slope = BIAS ? a.slopes[at.head] * kLog2e : 0.f;
         score.init(a);
         load_row<T, D>(static_cast<const T *>(a.q) + at.row * a.q_s[0] + at.head * a.q_s[1], a.dim, h, q);
@@ -115,7 +116,7 @@ struct Columns {
     // be multiplied by.
     template <int NB>
     __device__ float weights(f32x16_t *x, typename M::Frag *p, int j0) {
-        const float away = place - float(j0) - 4.f * h;
+        const float away = float(place - j0 - 4 * h);
         const int left = limit - j0 - 4 * h;
         float top = -kInf;
 #pragma unroll
@@ -263,7 +264,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_tiles(AttnArgs 
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) read(i);
             __builtin_amdgcn_sched_barrier(0);
-            const float away = col.place - float(now * N) - 4.f * col.h;
+            const float away = float(col.place - now * N - 4 * col.h);
             float top = -kInf, base = 0.f, less = 1.f, sum = 0.f;
             // plain scores: the maximum first, the weights beside all products;
             // others: the scores beside the first half, the weights beside the

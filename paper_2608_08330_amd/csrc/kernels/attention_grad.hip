@@ -113,7 +113,7 @@ __global__ __launch_bounds__(256, (kWavesDq<T, D>)) void k_dq(AttnArgs a, float 
     delta = half_sum(delta);
     const int64_t stat = int64_t(at.head) * a.q_rows + at.row;
     float base = base_of(a.lse[stat]);
-    const float place = float(sq.nk - sq.nq + at.i);
+    const int place = sq.nk - sq.nq + at.i;
     const float slope = BIAS ? a.slopes[at.head] * kLog2e : 0.f;
     Score score;
     score.init(a);
@@ -158,7 +158,7 @@ __global__ __launch_bounds__(256, (kWavesDq<T, D>)) void k_dq(AttnArgs a, float 
         for (int kk = 0; kk < D / 16; ++kk) x = M::mma(from.row_frag(0, 0, kk), q[kk], x);
 #pragma unroll
         for (int kk = 0; kk < D / 16; ++kk) dp = M::mma(from.row_frag(kBytes, 0, kk), g[kk], dp);
-        const float away = place - float(j0) - 4.f * h;
+        const float away = float(place - j0 - 4 * h);
         const int left = limit - j0 - 4 * h;
         if (j0 == 0 && first_limit <= 32) {
             float p[16], top = -kInf, sum = 0.f, dot = 0.f;
@@ -212,7 +212,7 @@ __global__ __launch_bounds__(256, (kWavesDq<T, D>)) void k_dq(AttnArgs a, float 
         typename M::Frag w0, w1;
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) read(i);
-        const float away = place - float(j0) - 4.f * h;
+        const float away = float(place - j0 - 4 * h);
 #pragma unroll
         for (int i = 0; i < 3 * H; ++i) {
             if (i < H) x = M::mma(f[i], q[i], x);

@@ -132,3 +132,33 @@ def test_weights_inside_a_larger_buffer(shift, weights, precision):
 
     for a, b in zip(run(0), run(shift)):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("nq", [2, 200])
+def test_distances_in_a_history_past_2_to_24(nq):
+    """The distance bias of queries at places that float32 does not hold: with
+    a slope of 0.7 the last 300 keys are all that counts (the others' weights
+    are below e^-70), and the oracle sees only those."""
+    import torch
+    dim, n, rows = 16, 300, (1 << 24) + 333
+    tail = Case("bf16", [(nq, n, 0)], 2, 1, dim, causal=True, bias=True, seed=nq)
+    tail.slopes = torch.full((2,), 0.7)
+    o = tail.oracle()
+    c = Case("bf16", [(nq, nq, 0)], 2, 1, dim, causal=True, bias=True, seed=nq)
+    c.q, c.do = tail.q, tail.do
+    c.k, c.v = (torch.zeros(rows, 1, dim, dtype=torch.bfloat16) for _ in range(2))
+    c.k[-n:], c.v[-n:] = tail.k, tail.v
+    c.lists.update(k_lens=torch.tensor([rows], dtype=torch.int32, device="cuda"),
+                   slopes=tail.slopes.cuda())
+    c.to_gpu().forward()
+    s, p = tail.errors()
+    lse, out = _f64(c.lse), _f64(c.out)
+    assert (np.abs(lse - o.lse) <= s + n * U + 2.0 ** -20 + 4 * U * np.abs(o.lse)).all()
+    assert (np.abs(out - o.out) <= (p + B) * o.out_abs + (B + U) * np.abs(o.out)).all()
+    c.backward()
+    grads, sizes = o.grad(_f64(c.do))
+    rel = p + (2 * dim + 16 + 2 * nq) * U + 3 * B
+    for got, want, size in ((c.dq, grads[0], sizes[0]), (c.dk[-n:], grads[1], sizes[1]), (c.dv[-n:], grads[2], sizes[2])):
+        assert (np.abs(_f64(got) - want) <= rel * size + (B + U) * np.abs(want) + 1e-30).all()
+    # keys further away: at most e^-70 of the queries' sizes
+    assert c.dk[:-n].abs().max().item() < 1e-20 and c.dv[:-n].abs().max().item() < 1e-20
