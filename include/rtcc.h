@@ -617,8 +617,8 @@ typedef struct rtcc_attn_desc {
     int32_t causal;               /* 0 or 1                                             */
     float scale;                  /* finite, > 0                                        */
     float softcap;                /* finite, >= 0; 0: no cap                            */
-    int64_t q_rows;               /* rows of q and out; q_rows * q_heads < 2^31         */
-    int64_t k_rows;               /* rows of k and v, < 2^31                            */
+    int64_t q_rows;               /* rows of q and out; q_rows * q_heads <= 2^31 - 256  */
+    int64_t k_rows;               /* rows of k and v, at most 2^31 - 256                */
     const int32_t *q_offsets;     /* device [n_seqs + 1]                                */
     const int32_t *k_offsets;     /* device [n_seqs], [n_seqs + 1] without k_lens       */
     const int32_t *k_lens;        /* device [n_seqs] or NULL                            */

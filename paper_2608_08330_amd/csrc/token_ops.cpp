@@ -14,6 +14,8 @@ void set_thread_error(const std::string &msg);
 namespace {
 
 constexpr int64_t kMaxRows = 2147483647;
+// Of attention: a place up to a tile past the last row is still an int.
+constexpr int64_t kMaxPlaces = 2147483648 - 256;
 // Between rows: 64 rows of a tile lie within 32-bit offsets of its first.
 constexpr int64_t kMaxRowStride = int64_t(1) << 22, kMaxHeadStride = int64_t(1) << 40;
 constexpr int32_t kMaxHeads = 1024, kMaxSeqs = 65536;
@@ -166,8 +168,8 @@ Checks check_attention(const rtcc_attn_desc &d, rtcc::kern::AttnArgs &a) {
     c.need(d.causal == 0 || d.causal == 1, "causal must be 0 or 1");
     c.need(std::isfinite(d.scale) && d.scale > 0.f, "scale must be finite and > 0");
     c.need(std::isfinite(d.softcap) && d.softcap >= 0.f, "softcap must be finite and >= 0");
-    c.need(d.q_rows >= 0 && d.q_rows <= kMaxRows / d.q_heads, "q_rows * q_heads out of range");
-    c.need(d.k_rows >= 0 && d.k_rows <= kMaxRows, "k_rows out of range");
+    c.need(d.q_rows >= 0 && d.q_rows <= kMaxPlaces / d.q_heads, "q_rows * q_heads out of range");
+    c.need(d.k_rows >= 0 && d.k_rows <= kMaxPlaces, "k_rows out of range");
     c.need(!d.prefix_lens || d.causal, "prefix_lens without causal");
     if (!c.why.empty()) return c;
     const int32_t elem = d.precision == RTCC_PREC_BF16 ? 2 : 4;

@@ -25,7 +25,7 @@ void check(const char *what, int64_t blocks, int threads) {
 }  // namespace
 
 int main() {
-    const int64_t kMax = 2147483647;  // rows; q_rows * q_heads too
+    const int64_t kMax = 2147483647;  // past all the limits of rows and q_rows * q_heads
     for (int heads : {1, 3, 256, 1024})
         for (int group : {1, 4, 1024}) {
             if (int64_t(heads) * group > 1024) continue;

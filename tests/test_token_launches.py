@@ -18,6 +18,15 @@ def test_launches_at_the_limits(tmp_path):
     assert r.returncode == 0, r.stdout
 
 
+def test_places_past_the_last_row_fit_an_int():
+    """A tile's rows are counted up to 127 past the last one."""
+    most = (1 << 31) - 256
+    for name in ("q_rows", "k_rows"):
+        for rows, status in ((most, R.RTCC_E_STATE), (most + 1, R.RTCC_E_ARG), ((1 << 31) - 1, R.RTCC_E_ARG)):
+            got, message = _status(R.rtcc_attention, _attn(q_heads=1, kv_heads=1, **{name: rows}), 0, 0)
+            assert got == status and (got != R.RTCC_E_ARG or name in message)
+
+
 def test_more_keys_than_the_gradient_counts_are_refused():
     p = _address()
     for kv_heads, rows, status in ((1024, (1 << 25) - 1, R.RTCC_E_STATE), (1024, 1 << 25, R.RTCC_E_ARG)):
