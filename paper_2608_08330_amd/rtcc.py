@@ -677,6 +677,12 @@ def norm_rope_desc(q, k, q_out, k_out, q_weight, k_weight, positions, inv_freq, 
     x = q if q is not None else k
     if x is None:
         raise ValueError("q and k are both None")
+    if x.ndim != 3:
+        raise ValueError("q and k must be [rows, heads, head_dim]")
+    if slots is not None and (k is None or k_out is None):
+        raise ValueError("slots are for k: k and k_out are needed")
+    if v is not None and (v_out is None or slots is None):
+        raise ValueError("v is copied by slots: slots and v_out are needed")
     rows, dim, dtype = x.shape[0], x.shape[2], x.dtype
     d.abi_version, d.precision, d.rows, d.head_dim = RTCC_ABI_VERSION, _precision_of(x), rows, dim
     d.interleaved, d.eps = int(bool(interleaved)), eps
@@ -719,6 +725,8 @@ def norm_rope_grad_desc(fwd, dq_out, dk_out, dq, dk, dq_weight=None, dk_weight=N
         for name in names:
             x = {"dq_out": dq_out, "dq": dq, "dk_out": dk_out, "dk": dk}[name]
             if heads:
+                if x is None:
+                    raise ValueError("%s is None" % name)
                 if _precision_of(x) != fwd.precision:
                     raise ValueError("%s must have the forward tensors' dtype" % name)
                 dtype = x.dtype
@@ -738,6 +746,9 @@ def attention_desc(q, k, v, out, q_offsets, k_offsets, k_lens=None, prefix_lens=
     slopes float32 [q_heads]; lse float32 [q_heads, q_rows].  scale: default
     1 / sqrt(head_dim)."""
     d = rtcc_attn_desc()
+    for name, x in (("q", q), ("k", k)):
+        if x.ndim != 3:
+            raise ValueError("%s must be [rows, heads, head_dim]" % name)
     rows, heads, dim = q.shape
     n = q_offsets.shape[0] - 1
     d.abi_version, d.precision, d.n_seqs = RTCC_ABI_VERSION, _precision_of(q), n

@@ -76,3 +76,19 @@ def test_host_tensors_reach_the_host_library_only():
         with pytest.raises(R.RtccError) as e:
             call(desc, *rest, kind="host")
         assert e.value.status == R.RTCC_E_STATE
+
+
+def test_missing_or_flat_tensors():
+    x, pos, f = torch.zeros(4, 2, 32), torch.zeros(4, 1), torch.zeros(16)
+    slots, off = torch.zeros(4, dtype=torch.int64), torch.tensor([0, 4], dtype=torch.int32)
+    rest = (None, None, pos, f, (16,))
+    for args, kw in (((x, None, x, None), dict(slots=slots)), ((x, x, x, None), dict(slots=slots)),
+                     ((x, x, x, x), dict(v=x, slots=slots)), ((x, x, x, x), dict(v=x, v_out=x)),
+                     ((x[0], x, x, x), {}), ((x[0, 0], None, x, None), {})):
+        with pytest.raises(ValueError):
+            R.norm_rope_desc(*args, *rest, **kw)
+    with pytest.raises(ValueError, match="dk is None"):
+        R.norm_rope_grad_desc(R.norm_rope_desc(x, x, x, x, *rest), x, x, x, None)
+    for q, k in ((x[0], x), (x, x[0]), (x, x[0, 0])):
+        with pytest.raises(ValueError, match="rows, heads"):
+            R.attention_desc(q, k, k, x, off, off)
