@@ -162,3 +162,92 @@ def test_distances_in_a_history_past_2_to_24(nq):
         assert (np.abs(_f64(got) - want) <= rel * size + (B + U) * np.abs(want) + 1e-30).all()
     # keys further away: at most e^-70 of the queries' sizes
     assert c.dk[:-n].abs().max().item() < 1e-20 and c.dv[:-n].abs().max().item() < 1e-20
+
+
+# Long enough that tiles which all columns see whole run in turns, several of
+# them.  "shares": few blocks, so the keys are cut into shares (three or more,
+# turns start past the first key in all but one) and joined; "one": short
+# sequences beside a long one, which keep every row to one share.
+TURNS = {
+    "shares": [(150, 700, 64), (131, 1333, 500)],
+    "one": [(300, 705, 250)] + [(33, 20, 5)] * 3,
+    "square": [(330, 330, 40), (530, 530, 0)],
+}
+TERMS = {"plain": {}, "cap": dict(softcap=3.0), "wide_cap": dict(softcap=1e3), "bias": dict(bias=True),
+         "cap_bias": dict(softcap=3.0, bias=True)}
+
+
+@pytest.mark.parametrize("precision", PRECISIONS)
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("terms", sorted(TERMS))
+@pytest.mark.parametrize("dim", [32, 64, 128])
+@pytest.mark.parametrize("seqs", sorted(TURNS))
+def test_whole_tiles(seqs, dim, terms, causal, precision):
+    """Forward and gradients where whole tiles run in turns, with every term."""
+    c = Case(precision, TURNS[seqs], 2, 1, dim, causal=causal, gap=3, **TERMS[terms])
+    o = c.oracle()
+    c.to_gpu().forward()
+    # shares need a workspace; without one there are none
+    assert (R.rtcc_attention_workspace(c.d) > 0) == (seqs != "one")
+    c.check_forward(o).backward().check_backward(o)
+
+
+@pytest.mark.parametrize("precision", PRECISIONS)
+@pytest.mark.parametrize("dim", [48, 96])
+def test_whole_tiles_of_padded_heads(dim, precision):
+    c = Case(precision, TURNS["shares"], 4, 2, dim, causal=True, layout="heads", gap=1)
+    o = c.oracle()
+    c.to_gpu().forward().check_forward(o).backward().check_backward(o)
+
+
+@pytest.mark.parametrize("precision", PRECISIONS)
+def test_caches_in_any_order(precision):
+    """Key ranges that lie in another order than the queries."""
+    c = Case(precision, [(70, 90, 3), (40, 300, 0), (5, 33, 33)], 2, 2, 64, causal=True, gap=7)
+    (a, na, ka, la, pa), (b, nb, kb, lb, pb), (d, nd, kd, ld, pd) = c.seqs
+    c.seqs = [(a, na, kd, ld, pa), (b, nb, ka, la, pb), (d, nd, kb, lb, pd)]
+    for name in ("k_offsets", "k_lens"):
+        x = c.lists[name]
+        c.lists[name] = x[[2, 0, 1]].contiguous()
+    o = c.oracle()
+    c.to_gpu().forward().check_forward(o).backward().check_backward(o)
+
+
+@pytest.mark.parametrize("precision", PRECISIONS)
+@pytest.mark.parametrize("lists", [
+    dict(q_offsets=[0, 10, 30, 2 ** 31 - 1], k_offsets=[0, 10, 2 ** 31 - 7], k_lens=[10, 20, 2 ** 31 - 1]),
+    dict(q_offsets=[-5, 30, 12, 36]), dict(k_offsets=[-9, 40, -2 ** 31]), dict(k_lens=[-1, 5, 1000]),
+    dict(q_offsets=[36, 0, 36, 0], k_offsets=[35, 1, 0], k_lens=[500, 500, 500]),
+    dict(prefix_lens=[2 ** 31 - 1, -2 ** 31, 7]),
+])
+def test_nothing_is_written_past_the_buffers(lists, precision):
+    """Whatever the lists hold: results lie inside larger buffers whose other
+    rows keep what they hold, forward and backward, in both kinds of kernels."""
+    import torch
+    for rows in ((10, 20, 6), (1, 1, 2)):
+        c = Case(precision, [(r, 3 * r, 1) for r in rows], 2, 1, 64, causal=True)
+        for name, values in lists.items():
+            if name != "prefix_lens" and rows != (10, 20, 6):
+                values = [v if abs(v) > 1000 else v // 10 for v in values]
+            c.lists[name] = torch.tensor(values, dtype=torch.int32, device="cuda")
+        c.to_gpu()
+        guard, held = 200, []
+
+        def inside(x):
+            """A tensor like x, of 7s, between rows of 5s that are to stay."""
+            flat = torch.full((x.numel() + 2 * guard * 64,), 5.0, dtype=x.dtype, device="cuda")
+            held.append((flat, x.numel()))
+            return flat[guard * 64:guard * 64 + x.numel()].view(x.shape).fill_(7.0)
+
+        out, lse, dq, dk, dv = (inside(x) for x in (c.q, c.lse, c.q, c.k, c.k))
+        d = R.attention_desc(c.gq, c.gk, c.gv, out, lse=lse, causal=True, scale=c.scale, **c.lists)
+        n = R.rtcc_attention_workspace(d)
+        space = inside(torch.empty(max(n // 4, 4)))
+        R.rtcc_attention(d, space.data_ptr(), n)
+        g = R.attention_grad_desc(d, c.gdo, dq, dk, dv)
+        n = R.rtcc_attention_grad_workspace(g)
+        space = inside(torch.empty(n // 4))
+        R.rtcc_attention_grad(g, space.data_ptr(), n)
+        torch.cuda.synchronize()
+        for flat, size in held:
+            assert (flat[:guard * 64] == 5).all() and (flat[guard * 64 + size:] == 5).all()
