@@ -274,8 +274,11 @@ struct Stager {
             off[n] = c * 16 < head_bytes ? row * row_bytes + c * 16 : 0x80000000u;
         }
     }
-    // Of load n.  Offsets of padding stay past every buffer: 2^31 and at most
-    // 96 rows of 2^24 bytes more.
+    // Of load n.  A tile's bytes stay below 2^31; offsets of padding stay past
+    // that: 2^31 and at most ROWS - kPass rows more, in 32 bits.
+    static constexpr int64_t kMaxRowBytes = kMaxRowStride * int64_t(sizeof(T));
+    static_assert((ROWS - 1) * kMaxRowBytes + L::kRowBytes <= (int64_t(1) << 31), "a tile past 32-bit offsets");
+    static_assert((int64_t(1) << 31) + (ROWS - kPass) * kMaxRowBytes < (int64_t(1) << 32), "padding wraps");
     __device__ uint32_t offset(int n) const { return kOne ? off[0] + uint32_t(n * kPass) * row_bytes : off[kOne ? 0 : n]; }
     // The wave's part of a tile.
     __device__ static uint32_t part(int thread) {

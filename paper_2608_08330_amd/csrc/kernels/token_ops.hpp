@@ -69,6 +69,9 @@ inline int64_t column_blocks(const AttnArgs &a, int per) {
 inline int64_t key_blocks(const AttnArgs &a, int per) {
     return (int64_t(a.k_rows) / per + a.n_seqs) * a.kv_heads;
 }
+// Between rows: up to 128 rows of a tile lie within 32-bit offsets of its first
+// (attention.hpp checks this).
+constexpr int64_t kMaxRowStride = int64_t(1) << 22;
 // Of the gradient's smallest tiles of a long batch (64 keys): 2^29 + 2^26 blocks.
 constexpr int64_t kMaxGradKeys = int64_t(1) << 35;  // k_rows * kv_heads
 

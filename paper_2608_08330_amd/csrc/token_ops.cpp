@@ -16,8 +16,7 @@ namespace {
 constexpr int64_t kMaxRows = 2147483647;
 // Of attention: a place up to a tile past the last row is still an int.
 constexpr int64_t kMaxPlaces = 2147483648 - 256;
-// Between rows: 64 rows of a tile lie within 32-bit offsets of its first.
-constexpr int64_t kMaxRowStride = int64_t(1) << 22, kMaxHeadStride = int64_t(1) << 40;
+constexpr int64_t kMaxRowStride = rtcc::kern::kMaxRowStride, kMaxHeadStride = int64_t(1) << 40;
 constexpr int32_t kMaxHeads = 1024, kMaxSeqs = 65536;
 
 // First failed check of a call; empty while all hold.
