@@ -543,8 +543,9 @@ RTCC_API rtcc_status rtcc_rotated_nms_noalloc(const float *device_records, int64
  * Appending to a cache: with slots (device int64 [rows]) row r of k goes to
  * row slots[r] of k_out, of slot_rows rows, and row r of v, if given, is
  * copied to the same row of v_out; a slot outside [0, slot_rows) is skipped.
- * Two rows with one slot: either may be kept.  Without slots row r goes to
- * row r.  q_out may be q, and k_out k without slots, with the same strides. */
+ * Of two rows with one slot either may be kept, head by head and for v apart:
+ * a cache's slots should differ.  Without slots row r goes to row r.  q_out may
+ * be q, and k_out k without slots, with the same strides. */
 typedef struct rtcc_norm_rope_desc {
     int32_t abi_version;          /* RTCC_ABI_VERSION                                   */
     int32_t precision;            /* rtcc_precision of q, k, v and the outputs          */
@@ -643,7 +644,8 @@ RTCC_API rtcc_status rtcc_attention(const rtcc_attn_desc *desc, void *workspace,
  * Key ranges of different sequences must not overlap (their sums would race:
  * undefined values).  Rows of q, k, v in no sequence are not written; a key
  * that no query sees gets 0.  bf16: the softmax weights and their gradients
- * are rounded to bf16 for the products. */
+ * are rounded to bf16 for the products, and delta = sum(dout out) of a query
+ * that sees more than 32 keys is taken from out as it was rounded. */
 typedef struct rtcc_attn_grad_desc {
     rtcc_attn_desc fwd;
     const void *dout;
