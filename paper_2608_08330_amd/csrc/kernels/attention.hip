@@ -42,8 +42,9 @@ struct Shares {
     int splits;
 };
 
-// One wave's 32 columns.
-template <typename T, int D, Cap CAP, bool BIAS>
+// One wave's 32 columns.  BEHIND: by how much (in log 2) a weight may pass 1
+// before the maximum follows.
+template <typename T, int D, Cap CAP, bool BIAS, int BEHIND>
 struct Columns {
     typedef Op<T> M;
     typedef Tile<T, D> L;
@@ -99,14 +100,14 @@ struct Columns {
     __device__ float factor() const { return CAP != kNone || BIAS ? 1.f : score.c1; }
 
     // Advances the running maximum past `top`, a tile's own in this half.  It
-    // follows only where it is left behind by more than 2^8 (any value will do
-    // while the weights stay in range), so that the output is rescaled a few
+    // follows only where it is left behind by more than 2^BEHIND (any value will
+    // do while the weights stay in range), so that the output is rescaled a few
     // times a row instead of once a tile.  base: what to subtract from
     // scores; returns the factor of the sums so far.
     __device__ float advance(float top, float &base) {
         top = half_max(top) * factor();
         const float before = m;
-        m = top > m + 8.f ? top : m;
+        m = top > m + float(BEHIND) ? top : m;
         base = m == -kInf ? 0.f : m;
         return __builtin_amdgcn_exp2f(before - base);
     }
@@ -213,7 +214,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 ? 2 : 1) void k_tiles(AttnArgs 
     const int mine = a.causal ? int((columns + kTileColumns - 1) / kTileColumns) - 1 - sq.tile : sq.tile;
     const int64_t c0 = int64_t(mine) * kTileColumns;
 
-    Columns<T, D, CAP, BIAS> col;
+    Columns<T, D, CAP, BIAS, 8> col;
     col.init(a, sq, kvh, c0 + wave * 32);
     const int64_t c_last = min(c0 + kTileColumns, columns) - 1;
     const int keys = limit_of(a, sq, int(c_last / a.group));
@@ -361,7 +362,7 @@ __global__ __launch_bounds__((64 * kFewWaves<T, D>), 1) void k_few(AttnArgs a, S
     const int kvh = head_of(a), wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int64_t columns = int64_t(sq.nq) * a.group, c0 = int64_t(sq.tile) * kFewColumns;
 
-    Columns<T, D, CAP, BIAS> col;
+    Columns<T, D, CAP, BIAS, 0> col;
     col.init(a, sq, kvh, c0);
     const int keys = col.last_limit;
     int t0, t1;

@@ -251,3 +251,31 @@ def test_nothing_is_written_past_the_buffers(lists, precision):
         torch.cuda.synchronize()
         for flat, size in held:
             assert (flat[:guard * 64] == 5).all() and (flat[guard * 64 + size:] == 5).all()
+
+
+@pytest.mark.parametrize("late", [False, True])
+def test_the_largest_weight_of_a_single_token_is_not_rounded(late):
+    """bf16, one query, one key that takes most of the weight, 1 to 7.9 powers
+    of 2 above the one before (in a tile 128 keys before or in its own): its
+    weight is 1 before the sums are divided, so the output carries its own rounding and
+    that of the other weights only."""
+    import torch
+    n, dim, count = 150, 64, 96
+    c = Case("bf16", [(1, n, 0)] * count, 2, 2, dim)
+    c.scale = 0.125
+    c.q.zero_()
+    c.q[..., 0] = 8.0
+    c.k.zero_()
+    c.k[..., 0] = -60.0
+    top = (torch.arange(1, count + 1) * 5.4 / count).bfloat16()
+    for s in range(count):
+        c.k[s * n + (0 if late else n - 2), :, 0] = 0.0
+        c.k[s * n + n - 1, :, 0] = top[s]
+    c.to_gpu().forward()
+    o = c.oracle()
+    got = _f64(c.out)
+    v = _f64(c.v).reshape(count, n, 2, dim)
+    less = np.exp(-_f64(top))[:, None, None]  # of the other key's weight and the largest one
+    other = less / (1 + less) * np.abs(v[:, 0 if late else n - 2])
+    p = 2 * (dim + 8) * U * 8 + n * U + 2.0 ** -20  # of a weight: scores of up to 60 are exact here
+    assert (np.abs(got - o.out) <= B * np.abs(o.out) + B * other + p * o.out_abs).all()
