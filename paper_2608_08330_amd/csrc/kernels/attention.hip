@@ -43,7 +43,11 @@ struct Shares {
 };
 
 // One wave's 32 columns.  BEHIND: by how much (in log 2) a weight may pass 1
-// before the maximum follows.
+// before the maximum follows.  At 0 a row's largest weight is 1 and not rounded
+// in bf16: single tokens, 0.20% off instead of 0.27% (512 keys), for 1.5% more
+// time (64 caches of up to 32,768 keys).  `tiles` rescales more columns in a
+// pipeline that waits for it: 8,192 causal, capped tokens, 6 heads of 128, take
+// 190 us at 0 and 180 us at 8, 0.19% and 0.22% off; it keeps 8.
 template <typename T, int D, Cap CAP, bool BIAS, int BEHIND>
 struct Columns {
     typedef Op<T> M;
@@ -107,7 +111,8 @@ struct Columns {
     __device__ float advance(float top, float &base) {
         top = half_max(top) * factor();
         const float before = m;
-        m = top > m + float(BEHIND) ? top : m;
+        if constexpr (BEHIND == 0) m = fmaxf(m, top);
+        else m = top > m + float(BEHIND) ? top : m;
         base = m == -kInf ? 0.f : m;
         return __builtin_amdgcn_exp2f(before - base);
     }
