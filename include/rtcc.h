@@ -644,8 +644,8 @@ RTCC_API rtcc_status rtcc_attention(const rtcc_attn_desc *desc, void *workspace,
  * Key ranges of different sequences must not overlap (their sums would race:
  * undefined values).  Rows of q, k, v in no sequence are not written; a key
  * that no query sees gets 0.  bf16: the softmax weights and their gradients
- * are rounded to bf16 for the products, and delta = sum(dout out) of a query
- * that sees more than 32 keys is taken from out as it was rounded. */
+ * are rounded to bf16 for the products, and for dq delta = sum(dout out) of a
+ * query that sees more than 32 keys is taken from out as it was rounded. */
 typedef struct rtcc_attn_grad_desc {
     rtcc_attn_desc fwd;
     const void *dout;

@@ -279,3 +279,26 @@ def test_the_largest_weight_of_a_single_token_is_not_rounded(late):
     other = less / (1 + less) * np.abs(v[:, 0 if late else n - 2])
     p = 2 * (dim + 8) * U * 8 + n * U + 2.0 ** -20  # of a weight: scores of up to 60 are exact here
     assert (np.abs(got - o.out) <= B * np.abs(o.out) + B * other + p * o.out_abs).all()
+
+
+@pytest.mark.parametrize("dim", [64, 128])
+def test_key_gradients_do_not_see_the_rounding_of_out(dim):
+    """bf16, values that differ by one step of bf16: dS is what those steps leave
+    of dP - delta, and a delta from the rounded output would be off by as much.
+    Scores are whole numbers times the scale, exact but for it."""
+    import torch
+    n = 200
+    c = Case("bf16", [(n, n, 0)], 2, 2, dim, causal=True)
+    c.q, c.k = c.q.sign(), c.k.sign()
+    c.scale = 0.1
+    steps = (c.v > 0).float() + torch.arange(dim) % 64
+    c.v = (1 + steps / 128).bfloat16()
+    o = c.oracle()
+    c.to_gpu().forward().backward()
+    (_dq, dk, _dv), (_sq, size, _sv) = o.grad(_f64(c.do))
+    rounded = np.zeros_like(dk)  # dS, each rounded to bf16
+    for h, row, keys, p, _lse, _x, bend in o.rows():
+        dp = o.v[keys, h] @ _f64(c.do)[row, h]
+        rounded[keys, h] += np.outer(np.abs(p * (dp - p @ dp)) * c.scale, np.abs(o.q[row, h]))
+    rel = 2 * (4 * U * c.scale * dim) + n * U + 2.0 ** -20 + (2 * dim + 16 + n) * U
+    assert (np.abs(_f64(c.dk) - dk) <= rel * size + B * rounded + (B + U) * np.abs(dk) + 1e-30).all()
