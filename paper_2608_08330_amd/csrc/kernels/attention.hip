@@ -19,10 +19,15 @@
 // Both take a share of a sequence's keys where whole sequences would leave
 // compute units idle; `join` then adds the shares up in a fixed order.
 //
-// Whole calls, bf16: 16,384 tokens, 6 heads of 64: 468 us (881 TFLOP/s), the
-// exponentials beside the products; 8,192 tokens, causal, capped, 6 heads of
-// 128: 179 us; one token against 64 caches of up to 32,768 keys, 2 heads of 128:
-// 178 us (3.4 TB/s).
+// bf16: the weights are rounded for their product with V, whose matrix
+// instruction takes bf16; outputs are 0.19 to 0.23% off 64-bit values, their own
+// rounding 0.17%.  Weights as the sum of two operands would take half as many
+// products again (few queries, 64 caches: 0.17%, 197 us instead of 181).
+//
+// Whole calls, bf16: 16,384 tokens, 6 heads of 64: 453 to 468 us (910 to 881
+// TFLOP/s), matrix cores busy 44%, the exponentials beside the products; 8,192
+// tokens, causal, capped, 6 heads of 128: 181 us; one token against 64 caches of
+// up to 32,768 keys, 2 heads of 128: 185 us (3.3 TB/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -44,7 +49,7 @@ struct Shares {
 
 // One wave's 32 columns.  BEHIND: by how much (in log 2) a weight may pass 1
 // before the maximum follows.  At 0 a row's largest weight is 1 and not rounded
-// in bf16: single tokens, 0.20% off instead of 0.27% (512 keys), for 1.5% more
+// in bf16: single tokens, 0.20% off instead of 0.27% (512 keys), for 2% more
 // time (64 caches of up to 32,768 keys).  `tiles` rescales more columns in a
 // pipeline that waits for it: 8,192 causal, capped tokens, 6 heads of 128, take
 // 190 us at 0 and 180 us at 8, 0.19% and 0.22% off; it keeps 8.

@@ -14,15 +14,18 @@
 //     row of one key has dS = 0).  It also writes each row's lse and delta for
 //     dkv, and by then the sum of P (dP - delta) has what delta was short of: dK
 //     does not see o's rounding.  dQ does, where few keys have most of the
-//     weight (0.29% off 64-bit values against 0.24%, four capped, biased
-//     histories): taking it out needs sum P K beside dS K, which made forward and
-//     gradients 10% (heads of 64) and 15% (128) slower.
+//     weight or the values have a large common part: 0.29% off 64-bit values,
+//     dK 0.24%, four capped, biased histories.  Taking it out needs sum P K
+//     beside dS K: 0.24%, forward and gradients 10% (heads of 64) and 15% (128)
+//     slower.  dS as the sum of two bf16 operands: 0.23%, 6% and 37% slower.
 //   dkv: 32 keys a wave, K and V rows in registers; the queries of the group's
 //     heads pass through LDS, head by head, scores Q K^T and dO V^T, with the
 //     keys as columns; dV and dK are accumulated as dO^T P and Q^T dS.  The
 //     sum over the heads of a group is the order of the walk.
 // Forward and gradients, bf16: four causal, capped, biased histories of up to
-// 4,096 tokens, 6 heads of 64: 404 us; vector work of five products' weights.
+// 4,096 tokens, 6 heads of 64: 409 us, of these dq 129 us, dkv 170 us, with the
+// matrix cores busy 18% of the time and vector work the rest.  dkv spills 21 to
+// 45 registers at heads of 64.
 #include <algorithm>
 #include <type_traits>
 
@@ -41,7 +44,10 @@ template <int S>
 constexpr int kRows = 32 * S;
 constexpr int kSide = 128;  // columns or keys of a block if its waves shared none
 
-// Two waves a SIMD where the registers of a wave allow it.
+// Two waves a SIMD, for dkv of wide heads and float32 one: they need up to all
+// 512 registers.  dq of bf16 heads of 128 spills 60 to 90 registers at two and is
+// faster all the same: forward and gradients of 2 x 8,192 causal tokens, 6 heads,
+// 1,426 us, at one wave 1,525 us.
 template <typename T, int D>
 constexpr int kWavesDq = sizeof(T) == 2 ? 2 : 1;
 template <typename T, int D>
