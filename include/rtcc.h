@@ -656,6 +656,97 @@ RTCC_API rtcc_status rtcc_attention_grad_workspace(const rtcc_attn_grad_desc *de
 RTCC_API rtcc_status rtcc_attention_grad(const rtcc_attn_grad_desc *desc, void *workspace, size_t workspace_bytes,
                                          void *hip_stream);
 
+/* Layer norm of a residual stream (rtcc_layer_norm).  For every row
+ *   s = x + residual           (residual NULL: s = x)
+ *   out = (s - mean(s)) / sqrt(mean((s - mean(s))^2) + eps) * weight + bias
+ * and sum_out, if given, is s.  out is computed from s before it is rounded.
+ * Tensors are [rows][channels] with an element stride between rows, channels
+ * contiguous, rows 16-byte aligned; channels is a multiple of 8, at most 16384.
+ * out and sum_out may each be x or residual, with the same stride, but not one
+ * another. */
+typedef struct rtcc_layer_norm_desc {
+    int32_t abi_version;          /* RTCC_ABI_VERSION                                   */
+    int32_t precision;            /* rtcc_precision of x, residual, sum_out, out        */
+    int64_t rows;                 /* 0 .. 2^31 - 1                                      */
+    int32_t channels;             /* a multiple of 8 in [8, 16384]                      */
+    float eps;                    /* finite, >= 0                                       */
+    const void *x, *residual;     /* residual: NULL: none                               */
+    void *sum_out, *out;          /* sum_out: NULL: not wanted                          */
+    int64_t x_stride, residual_stride, sum_out_stride, out_stride;
+    const float *weight, *bias;   /* [channels], at any float's address; NULL: 1, 0     */
+} rtcc_layer_norm_desc;
+RTCC_API rtcc_status rtcc_layer_norm(const rtcc_layer_norm_desc *desc, void *hip_stream);
+
+/* Gradients of rtcc_layer_norm.  fwd describes the forward call; of its tensors
+ * only the normed one (sum_out where a residual is given, as it was rounded,
+ * and required then; else x) and weight are read.  dout: the gradient of out;
+ * dsum, if given, the gradient that reaches the sum past the norm.  dx: the
+ * gradient of x, and of residual alike, dsum added; it may be dout or dsum or
+ * the normed tensor, with the same stride.  dweight, dbias: float32 [channels],
+ * written, not added to; summed over the rows in a fixed order; NULL: not
+ * wanted.  workspace: device memory of at least rtcc_layer_norm_grad_workspace
+ * bytes, 16-byte aligned (NULL where that is 0); it needs no initial contents. */
+typedef struct rtcc_layer_norm_grad_desc {
+    rtcc_layer_norm_desc fwd;
+    const void *dout, *dsum;
+    void *dx;
+    int64_t dout_stride, dsum_stride, dx_stride;
+    float *dweight, *dbias;
+} rtcc_layer_norm_grad_desc;
+RTCC_API rtcc_status rtcc_layer_norm_grad_workspace(const rtcc_layer_norm_grad_desc *desc, size_t *bytes);
+RTCC_API rtcc_status rtcc_layer_norm_grad(const rtcc_layer_norm_grad_desc *desc, void *workspace,
+                                          size_t workspace_bytes, void *hip_stream);
+
+typedef enum rtcc_activation {
+    RTCC_ACT_SILU = 0,            /* z / (1 + exp(-z))                                  */
+    RTCC_ACT_GELU = 1             /* z (1 + erf(z / sqrt 2)) / 2                        */
+} rtcc_activation;
+
+/* Gated feed-forward unit (rtcc_gated_ffn).  For every row
+ *   g = w_gate x, u = w_up x, h = activation(g) u, out = w_down h
+ * Tensors are [rows][channels or hidden] with an element stride between rows as
+ * in rtcc_layer_norm, the weights [hidden][channels], [hidden][channels] and
+ * [channels][hidden] (each output's weights contiguous): w_gate and w_up may be
+ * the halves of one matrix.  channels and hidden are multiples of 8.
+ * gate, up, act: [rows][hidden] of one stride, what the gradients read of the
+ * forward call (g, u and h); all of them or none.  Without them h is held in the
+ * workspace.  bf16: h is rounded to bf16 for the product with w_down; g and u
+ * are rounded only where they are stored. */
+typedef struct rtcc_gated_ffn_desc {
+    int32_t abi_version;          /* RTCC_ABI_VERSION                                   */
+    int32_t precision;            /* rtcc_precision of all tensors                      */
+    int64_t rows;                 /* 0 .. 2^31 - 256                                    */
+    int32_t channels, hidden;     /* multiples of 8 in [8, 65536]                       */
+    int32_t activation;           /* rtcc_activation                                    */
+    const void *x, *w_gate, *w_up, *w_down;
+    void *out;
+    void *gate, *up, *act;
+    int64_t x_stride, w_gate_stride, w_up_stride, w_down_stride, out_stride;
+    int64_t hidden_stride;        /* of gate, up and act                                */
+} rtcc_gated_ffn_desc;
+/* workspace: device memory of at least rtcc_gated_ffn_workspace bytes, 16-byte
+ * aligned (NULL where that is 0); it needs no initial contents. */
+RTCC_API rtcc_status rtcc_gated_ffn_workspace(const rtcc_gated_ffn_desc *desc, size_t *bytes);
+RTCC_API rtcc_status rtcc_gated_ffn(const rtcc_gated_ffn_desc *desc, void *workspace, size_t workspace_bytes,
+                                    void *hip_stream);
+
+/* Gradients of rtcc_gated_ffn with respect to x and the weights.  fwd describes
+ * the forward call, whose gate, up and act (required) are read as they were
+ * rounded; its out is ignored.  dout: as out.  dx, dw_gate, dw_up, dw_down: as
+ * x and the weights; written, not added to (no rows: the weights' are 0); NULL:
+ * not wanted.  Every sum is in a fixed order: the results of two calls are the
+ * same bits.  bf16: the gradients of g and u are rounded to bf16 for the
+ * products with the weights and with x. */
+typedef struct rtcc_gated_ffn_grad_desc {
+    rtcc_gated_ffn_desc fwd;
+    const void *dout;
+    void *dx, *dw_gate, *dw_up, *dw_down;
+    int64_t dout_stride, dx_stride, dw_gate_stride, dw_up_stride, dw_down_stride;
+} rtcc_gated_ffn_grad_desc;
+RTCC_API rtcc_status rtcc_gated_ffn_grad_workspace(const rtcc_gated_ffn_grad_desc *desc, size_t *bytes);
+RTCC_API rtcc_status rtcc_gated_ffn_grad(const rtcc_gated_ffn_grad_desc *desc, void *workspace,
+                                         size_t workspace_bytes, void *hip_stream);
+
 /* ------------------------------------------------------------------------
  * Host-side models of the communication and of the profiled DAG.  They run
  * on the host only (no GPU work, no context), are deterministic, and report

@@ -38,6 +38,8 @@ HIP_SOURCES = [
     "kernels/norm_rope.hip",
     "kernels/attention.hip",
     "kernels/attention_grad.hip",
+    "kernels/layer_norm.hip",
+    "kernels/gated_ffn.hip",
     "nms_api.hip",
     "nms_noalloc.hip",
 ]

@@ -184,6 +184,13 @@ size_t attention_workspace(const AttnArgs &) { return 0; }
 int attention(const AttnArgs &, void *) { return -1; }
 size_t attention_grad_workspace(const AttnArgs &) { return 0; }
 int attention_grad(const AttnArgs &, void *) { return -1; }
+int layer_norm(const LayerNormArgs &, void *) { return -1; }
+size_t layer_norm_grad_workspace(const LayerNormArgs &) { return 0; }
+int layer_norm_grad(const LayerNormArgs &, void *) { return -1; }
+size_t gated_ffn_workspace(const FfnArgs &) { return 0; }
+int gated_ffn(const FfnArgs &, void *) { return -1; }
+size_t gated_ffn_grad_workspace(const FfnArgs &) { return 0; }
+int gated_ffn_grad(const FfnArgs &, void *) { return -1; }
 const char *launch_error(int) { return nullptr; }
 }  // namespace kern
 }  // namespace rtcc

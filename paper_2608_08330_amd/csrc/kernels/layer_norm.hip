@@ -1,0 +1,367 @@
+// Layer norm of a residual stream on gfx950, and its gradient.
+//
+//   s = x + residual,  n = (s - mean(s)) r,  r = 1 / sqrt(var(s) + eps),
+//   y = n w + b
+//   g = dy w;  ds = r (g - mean(g) - n mean(g n)) + dsum
+//   dw = sum over rows of dy n,  db = sum over rows of dy
+//
+// G threads hold one row in registers, V times eight channels each (thread l:
+// channels 8 (l + G v) ..), so every tensor is read once and the variance is the
+// mean square of what is left without the mean.  Rows of up to 2,048 channels
+// stay within a wave (G <= 64: sums by exchanges), longer ones take a block of
+// 256 or 512 threads (sums through LDS).  Bandwidth bound.
+#include <algorithm>
+
+#include <hip/hip_runtime.h>
+
+#include "compute_units.hpp"
+#include "token_ops.hpp"
+
+namespace rtcc {
+namespace kern {
+
+namespace {
+
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef float f32x4_any_t __attribute__((ext_vector_type(4), aligned(4)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+
+// 8 consecutive elements as they lie in memory, so that a row's loads are all
+// under way before the first is used
+template <typename T>
+struct Eight;
+template <>
+struct Eight<uint16_t> {
+    u32x4_t u;
+    __device__ void load(const uint16_t *p) { u = *reinterpret_cast<const u32x4_t *>(p); }
+    __device__ float operator[](int e) const {
+        return __uint_as_float(e & 1 ? u[e / 2] & 0xffff0000u : u[e / 2] << 16);
+    }
+};
+template <>
+struct Eight<float> {
+    f32x4_t a, b;
+    __device__ void load(const float *p) {
+        a = reinterpret_cast<const f32x4_t *>(p)[0];
+        b = reinterpret_cast<const f32x4_t *>(p)[1];
+    }
+    __device__ float operator[](int e) const { return e < 4 ? a[e] : b[e - 4]; }
+};
+__device__ inline void store8(uint16_t *p, const float *v) {
+    bf16x8_t f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) f[e] = __bf16(v[e]);
+    *reinterpret_cast<bf16x8_t *>(p) = f;
+}
+__device__ inline void store8(float *p, const float *v) {
+    f32x4_t a, b;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) a[e] = v[e], b[e] = v[e + 4];
+    reinterpret_cast<f32x4_t *>(p)[0] = a;
+    reinterpret_cast<f32x4_t *>(p)[1] = b;
+}
+// of a weight: float32 at any address of a float
+__device__ inline void load8_weight(const float *p, float *v) {
+    const f32x4_any_t a = reinterpret_cast<const f32x4_any_t *>(p)[0], b = reinterpret_cast<const f32x4_any_t *>(p)[1];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = a[e], v[e + 4] = b[e];
+}
+
+// Sums of N values over the G threads of a row; `part` is LDS of a block's waves
+// (G > 64), used again only after the caller's next barrier.
+template <int G, int N>
+__device__ inline void row_sums(float (&x)[N], float (*part)[2]) {
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int d = 1; d < (G < 64 ? G : 64); d <<= 1) x[n] += __shfl_xor(x[n], d);
+    if constexpr (G > 64) {
+        const int wave = threadIdx.x / 64;
+        if (threadIdx.x % 64 == 0)
+#pragma unroll
+            for (int n = 0; n < N; ++n) part[wave][n] = x[n];
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            x[n] = 0.f;
+#pragma unroll
+            for (int w = 0; w < G / 64; ++w) x[n] += part[w][n];
+        }
+    }
+}
+
+template <int G>
+constexpr int kThreads = G > 256 ? G : 256;
+
+template <typename T, int G, int V>
+__global__ __launch_bounds__(kThreads<G>) void k_layer_norm(LayerNormArgs a) {
+    constexpr int kRows = kThreads<G> / G;
+    __shared__ float part[2][G > 64 ? G / 64 : 1][2];
+    const uint32_t place = (blockIdx.z * gridDim.x + blockIdx.x) * uint32_t(kRows) + threadIdx.x / G;
+    if (place >= uint32_t(a.rows)) return;  // all of a row's threads
+    const int64_t row = place;
+    const int l = threadIdx.x % G;
+    const float over = 1.f / float(a.channels);
+    Eight<T> x[V], r[V];
+    const T *px = static_cast<const T *>(a.x) + row * a.x_s, *pr = static_cast<const T *>(a.residual) + row * a.residual_s;
+    float s[V][8], sum[1] = {}, square[1] = {};
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int c = 8 * (l + G * v);
+        if (c < a.channels) {
+            x[v].load(px + c);
+            if (a.residual) r[v].load(pr + c);
+        }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const bool on = 8 * (l + G * v) < a.channels;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            s[v][e] = on ? (a.residual ? x[v][e] + r[v][e] : x[v][e]) : 0.f;
+            sum[0] += s[v][e];
+        }
+        if (on && a.sum_out) store8(static_cast<T *>(a.sum_out) + row * a.sum_s + 8 * (l + G * v), s[v]);
+    }
+    row_sums<G>(sum, part[0]);
+    const float mean = sum[0] * over;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            s[v][e] = 8 * (l + G * v) < a.channels ? s[v][e] - mean : 0.f;
+            square[0] = fmaf(s[v][e], s[v][e], square[0]);
+        }
+    row_sums<G>(square, part[1]);
+    const float scale = rsqrtf(fmaf(square[0], over, a.eps));
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int c = 8 * (l + G * v);
+        if (c >= a.channels) continue;
+        float w[8], b[8];
+        if (a.weight) load8_weight(a.weight + c, w);
+        if (a.bias) load8_weight(a.bias + c, b);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            s[v][e] *= scale;
+            s[v][e] = fmaf(s[v][e], a.weight ? w[e] : 1.f, a.bias ? b[e] : 0.f);
+        }
+        store8(static_cast<T *>(a.out) + row * a.out_s + c, s[v]);
+    }
+}
+
+// A block walks rows and keeps the sums of its channels' dw and db in registers;
+// partial: [blocks][2][channels].
+template <typename T, int G, int V>
+__global__ __launch_bounds__(kThreads<G>) void k_layer_norm_grad(LayerNormArgs a) {
+    constexpr int kRows = kThreads<G> / G;
+    __shared__ float part[3][G > 64 ? G / 64 : 1][2];
+    const int l = threadIdx.x % G;
+    const float over = 1.f / float(a.channels);
+    float dw[V][8] = {}, db[V][8] = {};
+    for (int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / G; row < a.rows; row += int64_t(gridDim.x) * kRows) {
+        Eight<T> x[V], dy[V], ds[V];
+        const T *px = static_cast<const T *>(a.x) + row * a.x_s, *pg = static_cast<const T *>(a.dout) + row * a.dout_s;
+        const T *pd = static_cast<const T *>(a.residual) + row * a.residual_s;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int c = 8 * (l + G * v);
+            if (c < a.channels) {
+                x[v].load(px + c);
+                dy[v].load(pg + c);
+                if (a.residual) ds[v].load(pd + c);
+            }
+        }
+        float n[V][8], sum[1] = {}, square[1] = {}, dots[2] = {};
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                n[v][e] = 8 * (l + G * v) < a.channels ? x[v][e] : 0.f;
+                sum[0] += n[v][e];
+            }
+        row_sums<G>(sum, part[0]);
+        const float mean = sum[0] * over;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                n[v][e] = 8 * (l + G * v) < a.channels ? n[v][e] - mean : 0.f;
+                square[0] = fmaf(n[v][e], n[v][e], square[0]);
+            }
+        row_sums<G>(square, part[1]);
+        const float scale = rsqrtf(fmaf(square[0], over, a.eps));
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int c = 8 * (l + G * v);
+            if (c >= a.channels) continue;
+            float w[8];
+            if (a.weight) load8_weight(a.weight + c, w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                n[v][e] *= scale;
+                const float g = a.weight ? dy[v][e] * w[e] : dy[v][e];
+                dw[v][e] = fmaf(dy[v][e], n[v][e], dw[v][e]);
+                db[v][e] += dy[v][e];
+                dots[0] += g;
+                dots[1] = fmaf(g, n[v][e], dots[1]);
+            }
+        }
+        row_sums<G>(dots, part[2]);
+        const float m0 = dots[0] * over, m1 = dots[1] * over;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int c = 8 * (l + G * v);
+            if (c >= a.channels) continue;
+            float w[8], y[8];
+            if (a.weight) load8_weight(a.weight + c, w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float g = a.weight ? dy[v][e] * w[e] : dy[v][e];
+                y[e] = scale * (g - fmaf(n[v][e], m1, m0));
+                if (a.residual) y[e] += ds[v][e];
+            }
+            store8(static_cast<T *>(a.out) + row * a.out_s + c, y);
+        }
+        if constexpr (G > 64) __syncthreads();  // the sums' LDS before the next row
+    }
+    if (!a.partial) return;
+    float *to = a.partial + int64_t(blockIdx.x) * 2 * a.channels;
+    if constexpr (G >= 256) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int c = 8 * (l + G * v);
+            if (c >= a.channels) continue;
+            store8(to + c, dw[v]);
+            store8(to + a.channels + c, db[v]);
+        }
+    } else {
+        // the rows of a wave, then the four waves
+        __shared__ float both[4][2][V * G * 8];
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+#pragma unroll
+                for (int d = G; d < 64; d <<= 1) {
+                    dw[v][e] += __shfl_xor(dw[v][e], d);
+                    db[v][e] += __shfl_xor(db[v][e], d);
+                }
+                if (threadIdx.x % 64 < G) {
+                    both[threadIdx.x / 64][0][8 * (l + G * v) + e] = dw[v][e];
+                    both[threadIdx.x / 64][1][8 * (l + G * v) + e] = db[v][e];
+                }
+            }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * a.channels; i += 256) {
+            const int k = i >= a.channels, c = i - k * a.channels;
+            to[i] = (both[0][k][c] + both[1][k][c]) + (both[2][k][c] + both[3][k][c]);
+        }
+    }
+}
+
+// Adds up the blocks' sums, in a fixed order: kSumThreads threads a channel take
+// every kSumThreads-th block, then halves are added.
+constexpr int kSumChannels = 16, kSumThreads = 64;
+__global__ __launch_bounds__(kSumChannels *kSumThreads) void k_layer_norm_sums(LayerNormArgs a, int blocks) {
+    __shared__ float part[kSumThreads][kSumChannels];
+    const int x = threadIdx.x % kSumChannels, l = threadIdx.x / kSumChannels;
+    const int at = int(blockIdx.x) * kSumChannels + x;  // 2 channels is a multiple of 16
+    float sum = 0.f;
+#pragma unroll 4
+    for (int b = l; b < blocks; b += kSumThreads) sum += a.partial[int64_t(b) * 2 * a.channels + at];
+    part[l][x] = sum;
+    for (int half = kSumThreads / 2; half > 0; half /= 2) {
+        __syncthreads();
+        if (l < half) part[l][x] += part[l + half][x];
+    }
+    if (l == 0) {
+        if (at < a.channels) {
+            if (a.dweight) a.dweight[at] = part[0][x];
+        } else if (a.dbias) {
+            a.dbias[at - a.channels] = part[0][x];
+        }
+    }
+}
+
+// Threads of a row and eights of channels each: the fewest threads that hold the
+// row in at most four.
+struct Cut {
+    int g, v;
+};
+Cut cut(int channels) {
+    const int eights = channels / 8;
+    for (int g : {8, 16, 32, 64, 256, 512})
+        if (eights <= 4 * g) return {g, (eights + g - 1) / g};
+    return {512, 4};  // not reached: channels <= 16384
+}
+
+int grad_blocks(const LayerNormArgs &a) {
+    const int per = std::max(1, 256 / cut(a.channels).g);
+    return int(std::min<int64_t>(row_tiles(a.rows, per), 4 * compute_units()));
+}
+
+template <typename T, int G, int V>
+hipError_t run(const LayerNormArgs &a, int grad_blocks, hipStream_t s) {
+    if (grad_blocks) {
+        k_layer_norm_grad<T, G, V><<<grad_blocks, kThreads<G>, 0, s>>>(a);
+    } else {
+        const Fold f = fold(row_tiles(a.rows, kThreads<G> / G), kThreads<G>);
+        k_layer_norm<T, G, V><<<dim3(f.x, 1, f.z), kThreads<G>, 0, s>>>(a);
+    }
+    return hipGetLastError();
+}
+
+template <typename T, int G>
+hipError_t run(const LayerNormArgs &a, int v, int grad_blocks, hipStream_t s) {
+    switch (v) {
+        case 1: return run<T, G, 1>(a, grad_blocks, s);
+        case 2: return run<T, G, 2>(a, grad_blocks, s);
+        case 3: return run<T, G, 3>(a, grad_blocks, s);
+        default: return run<T, G, 4>(a, grad_blocks, s);
+    }
+}
+
+template <typename T>
+hipError_t run(const LayerNormArgs &a, int grad_blocks, hipStream_t s) {
+    const Cut c = cut(a.channels);
+    switch (c.g) {
+        case 8: return run<T, 8>(a, c.v, grad_blocks, s);
+        case 16: return run<T, 16>(a, c.v, grad_blocks, s);
+        case 32: return run<T, 32>(a, c.v, grad_blocks, s);
+        case 64: return run<T, 64>(a, c.v, grad_blocks, s);
+        case 256: return run<T, 256>(a, c.v, grad_blocks, s);
+        default: return run<T, 512>(a, c.v, grad_blocks, s);
+    }
+}
+
+}  // namespace
+
+int layer_norm(const LayerNormArgs &a, void *stream) {
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    return a.bf16 ? run<uint16_t>(a, 0, s) : run<float>(a, 0, s);
+}
+
+size_t layer_norm_grad_workspace(const LayerNormArgs &a) {
+    if (a.rows == 0 || !(a.dweight || a.dbias)) return 0;
+    return size_t(grad_blocks(a)) * 2 * a.channels * sizeof(float);
+}
+
+int layer_norm_grad(const LayerNormArgs &args, void *stream) {
+    LayerNormArgs a = args;
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    const bool sums = a.dweight || a.dbias;
+    if (!sums) a.partial = nullptr;
+    const int blocks = a.rows > 0 ? grad_blocks(a) : 0;  // the sums over no rows are zero
+    if (blocks) {
+        const hipError_t e = a.bf16 ? run<uint16_t>(a, blocks, s) : run<float>(a, blocks, s);
+        if (e != hipSuccess) return e;
+    }
+    if (!sums) return hipSuccess;
+    k_layer_norm_sums<<<2 * a.channels / kSumChannels, kSumChannels * kSumThreads, 0, s>>>(a, blocks);
+    return hipGetLastError();
+}
+
+}  // namespace kern
+}  // namespace rtcc

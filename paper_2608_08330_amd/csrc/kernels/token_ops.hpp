@@ -1,5 +1,5 @@
 // Arguments and launchers of the token operators (norm_rope.hip,
-// attention.hip, attention_grad.hip).  Host code only, free of HIP headers so
+// attention.hip, attention_grad.hip, layer_norm.hip, gated_ffn.hip).  Host code only, free of HIP headers so
 // that the argument checks build into the host test library, which has
 // launchers of its own that refuse.  A launcher checks nothing: token_ops.cpp
 // has validated the descriptor.  Return value: a hipError_t as int.
@@ -49,6 +49,33 @@ struct AttnArgs {
     void *workspace;
 };
 
+struct LayerNormArgs {
+    bool bf16;
+    int32_t rows, channels;
+    float eps;
+    // forward: x (+ residual) -> sum_out, out; gradient: x (the normed tensor),
+    // dout (+ dsum) -> out (dx).  Element strides between rows.
+    const void *x, *residual, *dout;
+    void *sum_out, *out;
+    int64_t x_s, residual_s, dout_s, sum_s, out_s;
+    const float *weight, *bias;
+    float *dweight, *dbias;
+    float *partial;  // gradient: [blocks][2][channels] sums
+};
+
+struct FfnArgs {
+    bool bf16, gelu;
+    int32_t rows, channels, hidden;
+    const void *x, *w_gate, *w_up, *w_down;
+    void *out, *gate, *up, *act;
+    int64_t x_s, w_gate_s, w_up_s, w_down_s, out_s, hidden_s;
+    // gradient
+    const void *dout;
+    void *dx, *dw_gate, *dw_up, *dw_down;
+    int64_t dout_s, dx_s, dw_gate_s, dw_up_s, dw_down_s;
+    void *workspace;
+};
+
 // Blocks of a launch, of which a kernel counts blockIdx.z * gridDim.x +
 // blockIdx.x: HIP takes fewer than 2^32 threads an axis.  The description's
 // limits keep every number of blocks below 2^31.
@@ -75,6 +102,10 @@ constexpr int64_t kMaxRowStride = int64_t(1) << 22;
 // Of the gradient's smallest tiles of a long batch (64 keys): 2^29 + 2^26 blocks.
 constexpr int64_t kMaxGradKeys = int64_t(1) << 35;  // k_rows * kv_heads
 
+// rows * width of the feed-forward unit: its tiles, of 64 x 64 values at least,
+// are fewer than 2^29 with the rounded ones.
+constexpr int64_t kMaxFfnValues = int64_t(1) << 40;
+
 size_t norm_rope_grad_workspace(const NormRopeArgs &a);
 int norm_rope(const NormRopeArgs &a, void *stream);
 int norm_rope_grad(const NormRopeArgs &a, void *stream);
@@ -82,6 +113,13 @@ size_t attention_workspace(const AttnArgs &a);
 int attention(const AttnArgs &a, void *stream);
 size_t attention_grad_workspace(const AttnArgs &a);
 int attention_grad(const AttnArgs &a, void *stream);
+int layer_norm(const LayerNormArgs &a, void *stream);
+size_t layer_norm_grad_workspace(const LayerNormArgs &a);
+int layer_norm_grad(const LayerNormArgs &a, void *stream);
+size_t gated_ffn_workspace(const FfnArgs &a);
+int gated_ffn(const FfnArgs &a, void *stream);
+size_t gated_ffn_grad_workspace(const FfnArgs &a);
+int gated_ffn_grad(const FfnArgs &a, void *stream);
 // Text of a launcher's error; null from the host test library's launchers.
 const char *launch_error(int e);
 

@@ -1,6 +1,8 @@
-// Entry points of the token operators (rtcc_norm_rope, rtcc_attention and
-// their gradients): argument checks and marshalling; the work is in
-// kernels/norm_rope.hip, attention.hip and attention_grad.hip.
+// Entry points of the token operators (rtcc_norm_rope, rtcc_attention,
+// rtcc_layer_norm, rtcc_gated_ffn and their gradients): argument checks and
+// marshalling; the work is in kernels/norm_rope.hip, attention.hip,
+// attention_grad.hip, layer_norm.hip and gated_ffn.hip.
+#include <algorithm>
 #include <cmath>
 #include <string>
 
@@ -18,6 +20,7 @@ constexpr int64_t kMaxRows = 2147483647;
 constexpr int64_t kMaxPlaces = 2147483648 - 256;
 constexpr int64_t kMaxRowStride = rtcc::kern::kMaxRowStride, kMaxHeadStride = int64_t(1) << 40;
 constexpr int32_t kMaxHeads = 1024, kMaxSeqs = 65536;
+constexpr int32_t kMaxNormChannels = 16384, kMaxFfnWidth = 65536;
 
 // First failed check of a call; empty while all hold.
 struct Checks {
@@ -40,6 +43,11 @@ struct Checks {
             else if (stride[i] * elem % 16)
                 why = std::string(name) + ": a stride breaks the 16-byte alignment of the heads";
         }
+    }
+    // [rows][width]
+    void matrix(const void *p, int64_t stride, int64_t rows, int32_t width, int32_t elem, const char *name) {
+        const int64_t both[2] = {stride, width};
+        tensor(p, both, rows, 1, width, elem, name);
     }
 };
 
@@ -232,6 +240,127 @@ Checks check_attention_grad(const rtcc_attn_grad_desc &d, rtcc::kern::AttnArgs &
     return c;
 }
 
+int64_t row_stride(int64_t stride, int64_t rows, int32_t width) { return rows > 1 ? stride : width; }
+
+// The part of a layer norm's call that forward and gradient share.
+Checks check_layer_norm(const rtcc_layer_norm_desc &d, rtcc::kern::LayerNormArgs &a) {
+    Checks c;
+    c.need(d.abi_version == RTCC_ABI_VERSION, "abi_version mismatch");
+    c.need(d.precision == RTCC_PREC_FP32 || d.precision == RTCC_PREC_BF16, "unknown precision");
+    c.need(d.rows >= 0 && d.rows <= kMaxRows, "rows out of range");
+    c.need(d.channels >= 8 && d.channels <= kMaxNormChannels && d.channels % 8 == 0,
+           "channels must be a multiple of 8 in [8, 16384]");
+    c.need(std::isfinite(d.eps) && d.eps >= 0.f, "eps must be finite and >= 0");
+    if (!c.why.empty()) return c;
+    a.bf16 = d.precision == RTCC_PREC_BF16;
+    a.rows = int32_t(d.rows);
+    a.channels = d.channels;
+    a.eps = d.eps;
+    a.weight = d.weight;
+    a.bias = d.bias;
+    return c;
+}
+
+Checks check_layer_norm_grad(const rtcc_layer_norm_grad_desc &d, rtcc::kern::LayerNormArgs &a) {
+    Checks c = check_layer_norm(d.fwd, a);
+    if (!c.why.empty()) return c;
+    const rtcc_layer_norm_desc &f = d.fwd;
+    const int32_t elem = a.bf16 ? 2 : 4;
+    if (f.residual) c.matrix(f.sum_out, f.sum_out_stride, f.rows, f.channels, elem, "sum_out");
+    else c.matrix(f.x, f.x_stride, f.rows, f.channels, elem, "x");
+    c.matrix(d.dout, d.dout_stride, f.rows, f.channels, elem, "dout");
+    if (d.dsum) c.matrix(d.dsum, d.dsum_stride, f.rows, f.channels, elem, "dsum");
+    c.matrix(d.dx, d.dx_stride, f.rows, f.channels, elem, "dx");
+    a.x = f.residual ? f.sum_out : f.x;
+    a.dout = d.dout;
+    a.residual = d.dsum;
+    a.out = d.dx;
+    a.x_s = row_stride(f.residual ? f.sum_out_stride : f.x_stride, f.rows, f.channels);
+    a.dout_s = row_stride(d.dout_stride, f.rows, f.channels);
+    a.residual_s = row_stride(d.dsum_stride, f.rows, f.channels);
+    a.out_s = row_stride(d.dx_stride, f.rows, f.channels);
+    a.dweight = d.dweight;
+    a.dbias = d.dbias;
+    return c;
+}
+
+Checks check_gated_ffn(const rtcc_gated_ffn_desc &d, rtcc::kern::FfnArgs &a) {
+    Checks c;
+    c.need(d.abi_version == RTCC_ABI_VERSION, "abi_version mismatch");
+    c.need(d.precision == RTCC_PREC_FP32 || d.precision == RTCC_PREC_BF16, "unknown precision");
+    c.need(d.rows >= 0 && d.rows <= kMaxPlaces, "rows out of range");
+    c.need(d.channels >= 8 && d.channels <= kMaxFfnWidth && d.channels % 8 == 0,
+           "channels must be a multiple of 8 in [8, 65536]");
+    c.need(d.hidden >= 8 && d.hidden <= kMaxFfnWidth && d.hidden % 8 == 0, "hidden must be a multiple of 8 in [8, 65536]");
+    c.need(d.activation == RTCC_ACT_SILU || d.activation == RTCC_ACT_GELU, "unknown activation");
+    if (!c.why.empty()) return c;
+    // blocks are counted in 31 bits
+    c.need(d.rows * std::max(d.channels, d.hidden) <= rtcc::kern::kMaxFfnValues, "rows * width out of range");
+    const int given = (d.gate != nullptr) + (d.up != nullptr) + (d.act != nullptr);
+    c.need(given == 0 || given == 3, "gate, up and act: all of them or none");
+    if (!c.why.empty()) return c;
+    const int32_t elem = d.precision == RTCC_PREC_BF16 ? 2 : 4;
+    c.matrix(d.x, d.x_stride, d.rows, d.channels, elem, "x");
+    c.matrix(d.w_gate, d.w_gate_stride, d.rows ? d.hidden : 0, d.channels, elem, "w_gate");
+    c.matrix(d.w_up, d.w_up_stride, d.rows ? d.hidden : 0, d.channels, elem, "w_up");
+    c.matrix(d.w_down, d.w_down_stride, d.rows ? d.channels : 0, d.hidden, elem, "w_down");
+    if (given) {
+        c.matrix(d.gate, d.hidden_stride, d.rows, d.hidden, elem, "gate");
+        c.matrix(d.up, d.hidden_stride, d.rows, d.hidden, elem, "up");
+        c.matrix(d.act, d.hidden_stride, d.rows, d.hidden, elem, "act");
+    }
+    a.bf16 = d.precision == RTCC_PREC_BF16;
+    a.gelu = d.activation == RTCC_ACT_GELU;
+    a.rows = int32_t(d.rows);
+    a.channels = d.channels;
+    a.hidden = d.hidden;
+    a.x = d.x;
+    a.w_gate = d.w_gate;
+    a.w_up = d.w_up;
+    a.w_down = d.w_down;
+    a.out = d.out;
+    a.gate = d.gate;
+    a.up = d.up;
+    a.act = d.act;
+    a.x_s = row_stride(d.x_stride, d.rows, d.channels);
+    a.w_gate_s = d.w_gate_stride;
+    a.w_up_s = d.w_up_stride;
+    a.w_down_s = d.w_down_stride;
+    a.out_s = row_stride(d.out_stride, d.rows, d.channels);
+    a.hidden_s = row_stride(d.hidden_stride, d.rows, d.hidden);
+    return c;
+}
+
+Checks check_gated_ffn_forward(const rtcc_gated_ffn_desc &d, rtcc::kern::FfnArgs &a) {
+    Checks c = check_gated_ffn(d, a);
+    if (c.why.empty()) c.matrix(d.out, d.out_stride, d.rows, d.channels, a.bf16 ? 2 : 4, "out");
+    return c;
+}
+
+Checks check_gated_ffn_grad(const rtcc_gated_ffn_grad_desc &d, rtcc::kern::FfnArgs &a) {
+    Checks c = check_gated_ffn(d.fwd, a);
+    if (!c.why.empty()) return c;
+    const rtcc_gated_ffn_desc &f = d.fwd;
+    const int32_t elem = a.bf16 ? 2 : 4;
+    c.need(f.gate || f.rows == 0, "gate, up and act are NULL");
+    c.matrix(d.dout, d.dout_stride, f.rows, f.channels, elem, "dout");
+    if (d.dx) c.matrix(d.dx, d.dx_stride, f.rows, f.channels, elem, "dx");
+    if (d.dw_gate) c.matrix(d.dw_gate, d.dw_gate_stride, f.hidden, f.channels, elem, "dw_gate");
+    if (d.dw_up) c.matrix(d.dw_up, d.dw_up_stride, f.hidden, f.channels, elem, "dw_up");
+    if (d.dw_down) c.matrix(d.dw_down, d.dw_down_stride, f.channels, f.hidden, elem, "dw_down");
+    a.dout = d.dout;
+    a.dx = d.dx;
+    a.dw_gate = d.dw_gate;
+    a.dw_up = d.dw_up;
+    a.dw_down = d.dw_down;
+    a.dout_s = row_stride(d.dout_stride, f.rows, f.channels);
+    a.dx_s = row_stride(d.dx_stride, f.rows, f.channels);
+    a.dw_gate_s = d.dw_gate_stride;
+    a.dw_up_s = d.dw_up_stride;
+    a.dw_down_s = d.dw_down_stride;
+    return c;
+}
+
 bool workspace_ok(const void *workspace, size_t given, size_t needed) {
     return needed == 0 || (workspace && given >= needed && reinterpret_cast<uintptr_t>(workspace) % 16 == 0);
 }
@@ -352,6 +481,112 @@ rtcc_status rtcc_attention_grad(const rtcc_attn_grad_desc *desc, void *workspace
         a.workspace = workspace;
         if (a.n_seqs == 0) return RTCC_OK;
         return launched(rtcc::kern::attention_grad(a, hip_stream), "rtcc_attention_grad");
+    });
+}
+
+rtcc_status rtcc_layer_norm(const rtcc_layer_norm_desc *desc, void *hip_stream) {
+    return guarded([&]() -> rtcc_status {
+        if (!desc) return fail(RTCC_E_ARG, "desc is NULL");
+        const rtcc_layer_norm_desc &d = *desc;
+        rtcc::kern::LayerNormArgs a{};
+        Checks c = check_layer_norm(d, a);
+        if (c.why.empty()) {
+            const int32_t elem = a.bf16 ? 2 : 4;
+            c.matrix(d.x, d.x_stride, d.rows, d.channels, elem, "x");
+            if (d.residual) c.matrix(d.residual, d.residual_stride, d.rows, d.channels, elem, "residual");
+            if (d.sum_out) c.matrix(d.sum_out, d.sum_out_stride, d.rows, d.channels, elem, "sum_out");
+            c.matrix(d.out, d.out_stride, d.rows, d.channels, elem, "out");
+            c.need(d.rows == 0 || d.out != d.sum_out, "out and sum_out are one tensor");
+            a.x = d.x;
+            a.residual = d.residual;
+            a.sum_out = d.sum_out;
+            a.out = d.out;
+            a.x_s = row_stride(d.x_stride, d.rows, d.channels);
+            a.residual_s = row_stride(d.residual_stride, d.rows, d.channels);
+            a.sum_s = row_stride(d.sum_out_stride, d.rows, d.channels);
+            a.out_s = row_stride(d.out_stride, d.rows, d.channels);
+        }
+        if (!c.why.empty()) return fail(RTCC_E_ARG, c.why);
+        if (d.rows == 0) return RTCC_OK;
+        return launched(rtcc::kern::layer_norm(a, hip_stream), "rtcc_layer_norm");
+    });
+}
+
+rtcc_status rtcc_layer_norm_grad_workspace(const rtcc_layer_norm_grad_desc *desc, size_t *bytes) {
+    return guarded([&]() -> rtcc_status {
+        if (!desc || !bytes) return fail(RTCC_E_ARG, "desc or bytes is NULL");
+        *bytes = 0;
+        rtcc::kern::LayerNormArgs a{};
+        const Checks c = check_layer_norm_grad(*desc, a);
+        if (!c.why.empty()) return fail(RTCC_E_ARG, c.why);
+        *bytes = rtcc::kern::layer_norm_grad_workspace(a);
+        return RTCC_OK;
+    });
+}
+
+rtcc_status rtcc_layer_norm_grad(const rtcc_layer_norm_grad_desc *desc, void *workspace, size_t workspace_bytes,
+                                 void *hip_stream) {
+    return guarded([&]() -> rtcc_status {
+        if (!desc) return fail(RTCC_E_ARG, "desc is NULL");
+        rtcc::kern::LayerNormArgs a{};
+        const Checks c = check_layer_norm_grad(*desc, a);
+        if (!c.why.empty()) return fail(RTCC_E_ARG, c.why);
+        if (!workspace_ok(workspace, workspace_bytes, rtcc::kern::layer_norm_grad_workspace(a)))
+            return fail(RTCC_E_ARG, kBadWorkspace);
+        a.partial = static_cast<float *>(workspace);
+        return launched(rtcc::kern::layer_norm_grad(a, hip_stream), "rtcc_layer_norm_grad");
+    });
+}
+
+rtcc_status rtcc_gated_ffn_workspace(const rtcc_gated_ffn_desc *desc, size_t *bytes) {
+    return guarded([&]() -> rtcc_status {
+        if (!desc || !bytes) return fail(RTCC_E_ARG, "desc or bytes is NULL");
+        *bytes = 0;
+        rtcc::kern::FfnArgs a{};
+        const Checks c = check_gated_ffn_forward(*desc, a);
+        if (!c.why.empty()) return fail(RTCC_E_ARG, c.why);
+        *bytes = rtcc::kern::gated_ffn_workspace(a);
+        return RTCC_OK;
+    });
+}
+
+rtcc_status rtcc_gated_ffn(const rtcc_gated_ffn_desc *desc, void *workspace, size_t workspace_bytes, void *hip_stream) {
+    return guarded([&]() -> rtcc_status {
+        if (!desc) return fail(RTCC_E_ARG, "desc is NULL");
+        rtcc::kern::FfnArgs a{};
+        const Checks c = check_gated_ffn_forward(*desc, a);
+        if (!c.why.empty()) return fail(RTCC_E_ARG, c.why);
+        if (!workspace_ok(workspace, workspace_bytes, rtcc::kern::gated_ffn_workspace(a)))
+            return fail(RTCC_E_ARG, kBadWorkspace);
+        a.workspace = workspace;
+        if (a.rows == 0) return RTCC_OK;
+        return launched(rtcc::kern::gated_ffn(a, hip_stream), "rtcc_gated_ffn");
+    });
+}
+
+rtcc_status rtcc_gated_ffn_grad_workspace(const rtcc_gated_ffn_grad_desc *desc, size_t *bytes) {
+    return guarded([&]() -> rtcc_status {
+        if (!desc || !bytes) return fail(RTCC_E_ARG, "desc or bytes is NULL");
+        *bytes = 0;
+        rtcc::kern::FfnArgs a{};
+        const Checks c = check_gated_ffn_grad(*desc, a);
+        if (!c.why.empty()) return fail(RTCC_E_ARG, c.why);
+        *bytes = rtcc::kern::gated_ffn_grad_workspace(a);
+        return RTCC_OK;
+    });
+}
+
+rtcc_status rtcc_gated_ffn_grad(const rtcc_gated_ffn_grad_desc *desc, void *workspace, size_t workspace_bytes,
+                                void *hip_stream) {
+    return guarded([&]() -> rtcc_status {
+        if (!desc) return fail(RTCC_E_ARG, "desc is NULL");
+        rtcc::kern::FfnArgs a{};
+        const Checks c = check_gated_ffn_grad(*desc, a);
+        if (!c.why.empty()) return fail(RTCC_E_ARG, c.why);
+        if (!workspace_ok(workspace, workspace_bytes, rtcc::kern::gated_ffn_grad_workspace(a)))
+            return fail(RTCC_E_ARG, kBadWorkspace);
+        a.workspace = workspace;
+        return launched(rtcc::kern::gated_ffn_grad(a, hip_stream), "rtcc_gated_ffn_grad");
     });
 }
 

@@ -34,6 +34,7 @@ RTCC_OK, RTCC_E_ARG, RTCC_E_STATE, RTCC_E_DUPLICATE, RTCC_E_MALFORMED = 0, 1, 2,
 RTCC_E_PREMATURE, RTCC_E_INFEASIBLE, RTCC_E_NOMEM, RTCC_E_HIP, RTCC_E_INTERNAL = 5, 6, 7, 8, 9
 RTCC_PREC_FP32, RTCC_PREC_BF16 = 0, 1
 RTCC_FUSE_MAX, RTCC_FUSE_ATTN = 0, 1
+RTCC_ACT_SILU, RTCC_ACT_GELU = 0, 1
 RTCC_MODE_RELEASE, RTCC_MODE_BARRIER = 0, 1
 RTCC_EXEC_PER_BRANCH_STREAMS, RTCC_EXEC_SERIAL = 0, 1
 RTCC_WAITING, RTCC_RELEASED, RTCC_RUNNING, RTCC_FINISHED = 0, 1, 2, 3
@@ -242,6 +243,60 @@ class rtcc_attn_grad_desc(ctypes.Structure):
     ]
 
 
+class rtcc_layer_norm_desc(ctypes.Structure):
+    _fields_ = [
+        ("abi_version", ctypes.c_int32),
+        ("precision", ctypes.c_int32),
+        ("rows", ctypes.c_int64),
+        ("channels", ctypes.c_int32),
+        ("eps", ctypes.c_float),
+        ("x", ctypes.c_void_p), ("residual", ctypes.c_void_p),
+        ("sum_out", ctypes.c_void_p), ("out", ctypes.c_void_p),
+        ("x_stride", ctypes.c_int64), ("residual_stride", ctypes.c_int64),
+        ("sum_out_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64),
+        ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+    ]
+
+
+class rtcc_layer_norm_grad_desc(ctypes.Structure):
+    _fields_ = [
+        ("fwd", rtcc_layer_norm_desc),
+        ("dout", ctypes.c_void_p), ("dsum", ctypes.c_void_p),
+        ("dx", ctypes.c_void_p),
+        ("dout_stride", ctypes.c_int64), ("dsum_stride", ctypes.c_int64), ("dx_stride", ctypes.c_int64),
+        ("dweight", ctypes.c_void_p), ("dbias", ctypes.c_void_p),
+    ]
+
+
+class rtcc_gated_ffn_desc(ctypes.Structure):
+    _fields_ = [
+        ("abi_version", ctypes.c_int32),
+        ("precision", ctypes.c_int32),
+        ("rows", ctypes.c_int64),
+        ("channels", ctypes.c_int32), ("hidden", ctypes.c_int32),
+        ("activation", ctypes.c_int32),
+        ("x", ctypes.c_void_p),
+        ("w_gate", ctypes.c_void_p), ("w_up", ctypes.c_void_p), ("w_down", ctypes.c_void_p),
+        ("out", ctypes.c_void_p),
+        ("gate", ctypes.c_void_p), ("up", ctypes.c_void_p), ("act", ctypes.c_void_p),
+        ("x_stride", ctypes.c_int64),
+        ("w_gate_stride", ctypes.c_int64), ("w_up_stride", ctypes.c_int64), ("w_down_stride", ctypes.c_int64),
+        ("out_stride", ctypes.c_int64),
+        ("hidden_stride", ctypes.c_int64),
+    ]
+
+
+class rtcc_gated_ffn_grad_desc(ctypes.Structure):
+    _fields_ = [
+        ("fwd", rtcc_gated_ffn_desc),
+        ("dout", ctypes.c_void_p),
+        ("dx", ctypes.c_void_p),
+        ("dw_gate", ctypes.c_void_p), ("dw_up", ctypes.c_void_p), ("dw_down", ctypes.c_void_p),
+        ("dout_stride", ctypes.c_int64), ("dx_stride", ctypes.c_int64),
+        ("dw_gate_stride", ctypes.c_int64), ("dw_up_stride", ctypes.c_int64), ("dw_down_stride", ctypes.c_int64),
+    ]
+
+
 EXPORTS = (
     "rtcc_create", "rtcc_read_checkpoint", "rtcc_create_from_checkpoint", "rtcc_destroy", "rtcc_set_mode", "rtcc_staging_buffer", "rtcc_begin_frame",
     "rtcc_release_branch", "rtcc_release_branch_device", "rtcc_release_branches", "rtcc_join_and_detect",
@@ -249,6 +304,8 @@ EXPORTS = (
     "rtcc_node_times", "rtcc_node_count", "rtcc_graph_stats", "rtcc_conv_plan", "rtcc_conv_tiling", "rtcc_rotated_nms", "rtcc_rotated_nms_noalloc", "rtcc_uplink_emulate", "rtcc_schedule_model",
     "rtcc_norm_rope", "rtcc_norm_rope_grad_workspace", "rtcc_norm_rope_grad",
     "rtcc_attention_workspace", "rtcc_attention", "rtcc_attention_grad_workspace", "rtcc_attention_grad",
+    "rtcc_layer_norm", "rtcc_layer_norm_grad_workspace", "rtcc_layer_norm_grad",
+    "rtcc_gated_ffn_workspace", "rtcc_gated_ffn", "rtcc_gated_ffn_grad_workspace", "rtcc_gated_ffn_grad",
     "rtcc_upward_rank", "rtcc_status_str", "rtcc_last_error",
 )
 
@@ -302,6 +359,15 @@ def _declare(lib):
         "rtcc_attention": (S, [ctypes.POINTER(rtcc_attn_desc), _P, ctypes.c_size_t, _P]),
         "rtcc_attention_grad_workspace": (S, [ctypes.POINTER(rtcc_attn_grad_desc), ctypes.POINTER(ctypes.c_size_t)]),
         "rtcc_attention_grad": (S, [ctypes.POINTER(rtcc_attn_grad_desc), _P, ctypes.c_size_t, _P]),
+        "rtcc_layer_norm": (S, [ctypes.POINTER(rtcc_layer_norm_desc), _P]),
+        "rtcc_layer_norm_grad_workspace": (S, [ctypes.POINTER(rtcc_layer_norm_grad_desc),
+                                               ctypes.POINTER(ctypes.c_size_t)]),
+        "rtcc_layer_norm_grad": (S, [ctypes.POINTER(rtcc_layer_norm_grad_desc), _P, ctypes.c_size_t, _P]),
+        "rtcc_gated_ffn_workspace": (S, [ctypes.POINTER(rtcc_gated_ffn_desc), ctypes.POINTER(ctypes.c_size_t)]),
+        "rtcc_gated_ffn": (S, [ctypes.POINTER(rtcc_gated_ffn_desc), _P, ctypes.c_size_t, _P]),
+        "rtcc_gated_ffn_grad_workspace": (S, [ctypes.POINTER(rtcc_gated_ffn_grad_desc),
+                                              ctypes.POINTER(ctypes.c_size_t)]),
+        "rtcc_gated_ffn_grad": (S, [ctypes.POINTER(rtcc_gated_ffn_grad_desc), _P, ctypes.c_size_t, _P]),
         "rtcc_uplink_emulate": (S, [ctypes.POINTER(rtcc_uplink_desc), _P, _P, _P, _P, _P]),
         "rtcc_schedule_model": (S, [ctypes.c_int32, _P, _P, ctypes.c_int64, ctypes.c_int32, _I64P, _I64P, _P]),
         "rtcc_upward_rank": (S, [ctypes.c_int32, _P, ctypes.c_int32, _P, _P]),
@@ -785,6 +851,95 @@ def attention_grad_desc(fwd, dout, dq, dk, dv):
     return g
 
 
+def _matrix(d, name, x, shape, dtype, stride=None):
+    """Fill the pointer and row stride of tensor `name` of description d, [rows,
+    width] with contiguous rows; None entries of shape are free."""
+    s = x.stride()
+    if len(s) != 2 or (s[1] != 1 and x.shape[1] > 1):
+        raise ValueError("%s must be [rows, width] with contiguous rows" % name)
+    if x.dtype != dtype:
+        raise ValueError("%s must have dtype %s" % (name, dtype))
+    if shape[0] not in (None, x.shape[0]) or shape[1] not in (None, x.shape[1]):
+        raise ValueError("%s must have shape %s" % (name, tuple(shape)))
+    _place(d, name, x)
+    setattr(d, stride or name + "_stride", s[0])
+
+
+def layer_norm_desc(x, out, weight=None, bias=None, residual=None, sum_out=None, eps=1e-5):
+    """Description of a layer norm of x (+ residual): x, residual, sum_out, out
+    [rows, channels]; weight, bias float32 [channels].  out may be None where only
+    the gradient is wanted."""
+    d = rtcc_layer_norm_desc()
+    if x.ndim != 2:
+        raise ValueError("x must be [rows, channels]")
+    dtype = x.dtype
+    d.abi_version, d.precision = RTCC_ABI_VERSION, _precision_of(x)
+    (d.rows, d.channels), d.eps = x.shape, eps
+    for name, t in (("x", x), ("residual", residual), ("sum_out", sum_out), ("out", out)):
+        if t is not None:
+            _matrix(d, name, t, x.shape, dtype)
+    for name, t in (("weight", weight), ("bias", bias)):
+        if t is not None:
+            _flat(d, name, t, (x.shape[1],), "torch.float32")
+    return d
+
+
+def layer_norm_grad_desc(fwd, dout, dx, dsum=None, dweight=None, dbias=None):
+    """Description of the gradients of the call that fwd (layer_norm_desc; with
+    its sum_out where it has a residual) describes; dsum: the gradient that
+    reaches the sum past the norm."""
+    g = _grad_of(rtcc_layer_norm_grad_desc, fwd)
+    if _precision_of(dout) != fwd.precision:
+        raise ValueError("dout must have the forward tensors' dtype")
+    for name, t in (("dout", dout), ("dsum", dsum), ("dx", dx)):
+        if t is not None:
+            _matrix(g, name, t, (fwd.rows, fwd.channels), dout.dtype)
+    for name, t in (("dweight", dweight), ("dbias", dbias)):
+        if t is not None:
+            _flat(g, name, t, (fwd.channels,), "torch.float32")
+    return g
+
+
+def gated_ffn_desc(x, w_gate, w_up, w_down, out, activation=RTCC_ACT_SILU, gate=None, up=None, act=None):
+    """Description of a gated feed-forward unit: x, out [rows, channels]; w_gate,
+    w_up [hidden, channels], w_down [channels, hidden]; gate, up, act [rows,
+    hidden] of one stride, for the gradients, or None.  out may be None where
+    only the gradients are wanted."""
+    d = rtcc_gated_ffn_desc()
+    if x.ndim != 2 or w_gate.ndim != 2:
+        raise ValueError("x must be [rows, channels] and w_gate [hidden, channels]")
+    (rows, channels), hidden, dtype = x.shape, w_gate.shape[0], x.dtype
+    d.abi_version, d.precision = RTCC_ABI_VERSION, _precision_of(x)
+    d.rows, d.channels, d.hidden, d.activation = rows, channels, hidden, activation
+    for name, t, shape in (("x", x, (rows, channels)), ("w_gate", w_gate, (hidden, channels)),
+                           ("w_up", w_up, (hidden, channels)), ("w_down", w_down, (channels, hidden)),
+                           ("out", out, (rows, channels))):
+        if t is not None or name != "out":
+            _matrix(d, name, t, shape, dtype)
+    first = None
+    for name, t in (("gate", gate), ("up", up), ("act", act)):
+        if t is not None:
+            _matrix(d, name, t, (rows, hidden), dtype, "hidden_stride")
+            if first not in (None, t.stride(0)) and rows > 1:
+                raise ValueError("gate, up and act must have one stride")
+            first = t.stride(0)
+    return d
+
+
+def gated_ffn_grad_desc(fwd, dout, dx=None, dw_gate=None, dw_up=None, dw_down=None):
+    """Description of the gradients of the call that fwd (gated_ffn_desc, with its
+    gate, up and act) describes; None: not wanted."""
+    g = _grad_of(rtcc_gated_ffn_grad_desc, fwd)
+    if _precision_of(dout) != fwd.precision:
+        raise ValueError("dout must have the forward tensors' dtype")
+    n, c, f = fwd.rows, fwd.channels, fwd.hidden
+    for name, t, shape in (("dout", dout, (n, c)), ("dx", dx, (n, c)), ("dw_gate", dw_gate, (f, c)),
+                           ("dw_up", dw_up, (f, c)), ("dw_down", dw_down, (c, f))):
+        if t is not None:
+            _matrix(g, name, t, shape, dout.dtype)
+    return g
+
+
 def _workspace_call(fn, desc, kind):
     lib = load(kind)
     n = ctypes.c_size_t()
@@ -830,6 +985,56 @@ def rtcc_attention_grad(desc, workspace, workspace_bytes, stream=0, kind="gpu"):
     _on_gpu(desc, kind)
     lib = load(kind)
     _free_call(lib, lib.rtcc_attention_grad(ctypes.byref(desc), _P(workspace), workspace_bytes, _P(stream)))
+
+
+def _on_current(d, kind):
+    """The kernels run on the current device: tensors of another are refused."""
+    _on_gpu(d, kind)
+    if kind == "gpu" and getattr(d, "device", -1) >= 0:
+        import torch
+        if torch.cuda.current_device() != d.device:
+            raise ValueError("the description's tensors are on device %d, the current device is %d"
+                             % (d.device, torch.cuda.current_device()))
+
+
+def rtcc_layer_norm(desc, stream=0, kind="gpu"):
+    """Layer norm of a residual stream (layer_norm_desc)."""
+    _on_current(desc, kind)
+    lib = load(kind)
+    _free_call(lib, lib.rtcc_layer_norm(ctypes.byref(desc), _P(stream)))
+
+
+def rtcc_layer_norm_grad_workspace(desc, kind="gpu"):
+    return _workspace_call("rtcc_layer_norm_grad_workspace", desc, kind)
+
+
+def rtcc_layer_norm_grad(desc, workspace, workspace_bytes, stream=0, kind="gpu"):
+    """Gradients of rtcc_layer_norm (layer_norm_grad_desc)."""
+    _on_current(desc, kind)
+    lib = load(kind)
+    _free_call(lib, lib.rtcc_layer_norm_grad(ctypes.byref(desc), _P(workspace), workspace_bytes, _P(stream)))
+
+
+def rtcc_gated_ffn_workspace(desc, kind="gpu"):
+    return _workspace_call("rtcc_gated_ffn_workspace", desc, kind)
+
+
+def rtcc_gated_ffn(desc, workspace, workspace_bytes, stream=0, kind="gpu"):
+    """Gated feed-forward unit (gated_ffn_desc)."""
+    _on_current(desc, kind)
+    lib = load(kind)
+    _free_call(lib, lib.rtcc_gated_ffn(ctypes.byref(desc), _P(workspace), workspace_bytes, _P(stream)))
+
+
+def rtcc_gated_ffn_grad_workspace(desc, kind="gpu"):
+    return _workspace_call("rtcc_gated_ffn_grad_workspace", desc, kind)
+
+
+def rtcc_gated_ffn_grad(desc, workspace, workspace_bytes, stream=0, kind="gpu"):
+    """Gradients of rtcc_gated_ffn (gated_ffn_grad_desc)."""
+    _on_current(desc, kind)
+    lib = load(kind)
+    _free_call(lib, lib.rtcc_gated_ffn_grad(ctypes.byref(desc), _P(workspace), workspace_bytes, _P(stream)))
 
 
 def _free_call(lib, st):
