@@ -87,6 +87,70 @@ struct Work {
 
 enum Epilogue { kPlain, kGated, kGatedGrad };
 
+// The product, the slice and the tile of a block.  Blocks of one XCD (every eighth)
+// take tiles that follow each other, in bands of kBand tiles of rows, so that their
+// operands meet in its L2.
+struct Spot {
+    int which, slice, tile_m, tile_n;  // which < 0: none, of a folded launch's last blocks
+};
+constexpr int kBand = 4;
+__device__ inline Spot spot(const Work &w) {
+    uint32_t id = blockIdx.z * gridDim.x + blockIdx.x;
+    int which = 0;
+    uint32_t tiles = w.p[0].tiles, across = w.p[0].tiles_n;
+#pragma unroll
+    for (int i = 1; i < kMaxProducts; ++i)
+        if (which == i - 1 && i < w.products && id >= tiles * w.slices) {
+            id -= tiles * w.slices;
+            which = i, tiles = w.p[i].tiles, across = w.p[i].tiles_n;
+        }
+    const uint32_t n = tiles * w.slices, x = id % 8;
+    if (id >= n) return {-1, 0, 0, 0};
+    id = x * (n / 8) + min(x, n % 8) + id / 8;
+    const int slice = int(id / tiles);
+    id %= tiles;
+    const uint32_t down = tiles / across, top = id / (kBand * across) * kBand, rows = min(down - top, uint32_t(kBand));
+    id -= top * across;
+    // said to be uniform, so that all addresses stay in scalar registers
+    return {__builtin_amdgcn_readfirstlane(which), __builtin_amdgcn_readfirstlane(slice),
+            __builtin_amdgcn_readfirstlane(top + id % rows), __builtin_amdgcn_readfirstlane(id / rows)};
+}
+// A copy by constant indexes: an indexed one would go through memory.
+__device__ inline Product pick(const Work &w, int which) { return which == 0 ? w.p[0] : which == 1 ? w.p[1] : w.p[2]; }
+
+// Stores four neighbouring results c (a gated product's: of gate, with those of up
+// in d) of row m from column n on.
+template <typename T, int EPI>
+__device__ inline void finish(const Work &w, const Product &p, int slice, int m, int n, f32x4_t c, f32x4_t d) {
+    if constexpr (EPI == kGated) {
+        const int64_t at = m * w.hidden_s + n;
+        f32x4_t h;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = activation(w.gelu, c[e], nullptr) * d[e];
+        store4(static_cast<T *>(w.act) + at, h);
+        if (w.gate) {
+            store4(static_cast<T *>(w.gate) + at, c);
+            store4(static_cast<T *>(w.up) + at, d);
+        }
+    } else if constexpr (EPI == kGatedGrad) {
+        const int64_t at = m * w.hidden_s + n, to = int64_t(m) * p.n + n;
+        const f32x4_t g = load4(static_cast<const T *>(w.gate) + at), u = load4(static_cast<const T *>(w.up) + at);
+        f32x4_t dg, du;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            float slope;
+            du[e] = c[e] * activation(w.gelu, g[e], &slope);
+            dg[e] = c[e] * u[e] * slope;
+        }
+        store4(static_cast<T *>(p.c) + to, dg);
+        store4(static_cast<T *>(p.c) + int64_t(p.m) * p.n + to, du);
+    } else if (w.slices > 1) {
+        store4(w.partial + slice * w.slice_size + p.partial + int64_t(m) * p.n + n, c);
+    } else {
+        store4(static_cast<T *>(p.c) + m * p.c_row + n, c);
+    }
+}
+
 // Columns of a tile lie in two halves of BN / 2 (of a gated product: of gate and
 // up).  Four waves, two by two.
 template <typename T, bool AK, bool BK, int EPI, int BM, int BN>
@@ -99,17 +163,11 @@ __global__ __launch_bounds__(256) void k_product(Work w) {
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave >> 1, wn = wave & 1;
-    uint32_t id = blockIdx.z * gridDim.x + blockIdx.x;
-    int which = 0;
-    for (; which < w.products; ++which) {
-        const uint32_t n = uint32_t(w.p[which].tiles) * w.slices;
-        if (id < n) break;
-        id -= n;
-    }
-    if (which == w.products) return;  // a folded launch's last blocks
-    const Product &p = w.p[which];
-    const int slice = int(id / uint32_t(p.tiles)), tile = int(id % uint32_t(p.tiles));
-    const int m0 = tile / p.tiles_n * BM, n0 = tile % p.tiles_n * (EPI == kGated ? BN / 2 : BN);
+    const Spot at_tile = spot(w);
+    if (at_tile.which < 0) return;
+    const Product p = pick(w, at_tile.which);
+    const int slice = at_tile.slice;
+    const int m0 = at_tile.tile_m * BM, n0 = at_tile.tile_n * (EPI == kGated ? BN / 2 : BN);
     const int steps = (p.k + kStep<T> - 1) / kStep<T>;
     const int first = slice * w.per_slice, last = min(first + w.per_slice, steps * w.segments);
 
@@ -121,7 +179,7 @@ __global__ __launch_bounds__(256) void k_product(Work w) {
         sa.init(threadIdx.x, p.a_row, int64_t(p.m - m0) * EL);
 #pragma unroll
         for (int h = 0; h < 2; ++h)
-            sb[h].init(threadIdx.x, p.b_row[EPI == kGated ? h : segment], int64_t(p.n - n0 - (EPI == kGated ? 0 : h * (BN / 2))) * EL);
+            sb[h].init(threadIdx.x, (EPI == kGated ? h : segment) ? p.b_row[1] : p.b_row[0], int64_t(p.n - n0 - (EPI == kGated ? 0 : h * (BN / 2))) * EL);
     };
     auto load = [&](int step, uint32_t to) {
         if (w.segments == 2 && segment == 0 && step >= steps) {
@@ -130,13 +188,13 @@ __global__ __launch_bounds__(256) void k_product(Work w) {
         }
         const int64_t k0 = int64_t(step - segment * steps) * kStep<T>;
         const int left = int(p.k - k0);
-        sa.load(p.a[segment] + (AK ? m0 * int64_t(p.a_row) + k0 * EL : k0 * p.a_row + int64_t(m0) * EL), p.a_row, p.m - m0,
+        sa.load((segment ? p.a[1] : p.a[0]) + (AK ? m0 * int64_t(p.a_row) + k0 * EL : k0 * p.a_row + int64_t(m0) * EL), p.a_row, p.m - m0,
                 left, to, part);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const uint32_t row = p.b_row[EPI == kGated ? h : segment];
+            const uint32_t row = (EPI == kGated ? h : segment) ? p.b_row[1] : p.b_row[0];
             const int at = n0 + (EPI == kGated ? 0 : h * (BN / 2));
-            const char *src = p.b[EPI == kGated ? h : segment];
+            const char *src = (EPI == kGated ? h : segment) ? p.b[1] : p.b[0];
             sb[h].load(src + (BK ? at * int64_t(row) + k0 * EL : k0 * row + int64_t(at) * EL), row, p.n - at, left,
                        to + PA::kBytes + h * PB::kBytes, part);
         }
@@ -179,50 +237,184 @@ __global__ __launch_bounds__(256) void k_product(Work w) {
     for (int i = 0; i < MT; ++i) {
         const int m = m0 + wm * (BM / 2) + 16 * i + fr;
         if (m >= p.m) continue;
-        if constexpr (EPI == kGated) {
+#pragma unroll
+        for (int h = 0; h < (EPI == kGated ? 1 : 2); ++h)
 #pragma unroll
             for (int j = 0; j < NT; ++j) {
-                const int n = n0 + wn * (BN / 4) + 16 * j + 4 * fk;
-                if (n >= p.n) continue;
-                const int64_t at = m * w.hidden_s + n;
-                const f32x4_t g = acc[i][0][j], u = acc[i][1][j];
-                f32x4_t h;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) h[e] = activation(w.gelu, g[e], nullptr) * u[e];
-                store4(static_cast<T *>(w.act) + at, h);
-                if (w.gate) {
-                    store4(static_cast<T *>(w.gate) + at, g);
-                    store4(static_cast<T *>(w.up) + at, u);
-                }
+                const int n = n0 + h * (BN / 2) + wn * (BN / 4) + 16 * j + 4 * fk;
+                if (n < p.n) finish<T, EPI>(w, p, slice, m, n, acc[i][h][j], acc[i][1][j]);
             }
-        } else {
+    }
+}
+
+// bf16, tiles of 256 x 256, eight waves of 128 x 64: rows 64 wm .. of both halves of
+// the tile's rows, columns 32 wn .. of both halves of its columns.  A step's four
+// panels (two halves of A, two of B) have two buffers.  A wave goes through a step in
+// four phases, each a quarter of its results:
+//   1: reads A0             products of A0, B0     (B0 is in registers)
+//   2: reads B1             products of A0, B1
+//   3: reads A1             products of A1, B1
+//   4: reads the next B0    products of A1, B0
+// A phase reads, waits, meets the other waves at a barrier, multiplies, and meets
+// them again.  Waves 4 .. 7 (the second wave of every SIMD) run one barrier behind,
+// so that on each SIMD one wave multiplies while the other reads.  A panel that
+// phase p has read is free in phase p + 1 and filled there with its values of two
+// steps later; loads are waited for one phase before they are read, with those of
+// the last six panels still under way.
+template <bool AK, bool BK, int EPI>
+__global__ __launch_bounds__(512) void k_product_large(Work w) {
+    typedef uint16_t T;
+    constexpr int EL = 2, BM = 256, BN = 256;
+    typedef Panel<T, AK, 128> PA;
+    typedef Panel<T, BK, 128> PB;
+    constexpr uint32_t kPanel = 128 * 128, kStage = 4 * kPanel;
+    constexpr uint32_t kA0 = 0, kA1 = kPanel, kB0 = 2 * kPanel, kB1 = 3 * kPanel;
+    __shared__ __attribute__((aligned(1024))) char lds[2 * kStage];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave >> 2, wn = wave & 3;
+    const Spot at_tile = spot(w);
+    if (at_tile.which < 0) return;
+    const Product p = pick(w, at_tile.which);
+    const int slice = at_tile.slice;
+    const int m0 = at_tile.tile_m * BM, n0 = at_tile.tile_n * (EPI == kGated ? BN / 2 : BN);
+    const int steps = (p.k + kStep<T> - 1) / kStep<T>;
+    const int first = slice * w.per_slice, last = min(first + w.per_slice, steps * w.segments);
+
+    const uint32_t base = lds_offset(lds), part = uint32_t(wave) * 1024u;
+    typename PA::template Stager<512> sa[2];
+    typename PB::template Stager<512> sb[2];
+    static_assert(sa[0].kLoads == 2 && sb[0].kLoads == 2, "the waits count two loads a panel");
+    auto aim_b = [&](int h, int segment) {
+        sb[h].init(threadIdx.x, (EPI == kGated ? h : segment) ? p.b_row[1] : p.b_row[0], int64_t(p.n - n0 - (EPI == kGated ? 0 : h * 128)) * EL);
+    };
+    // The panels of half h in the buffer `to`; past the slice's end nothing is
+    // fetched and zeros are stored, so that the number of loads stays the same.
+    auto load_a = [&](int h, int step, uint32_t to) {
+        const int segment = w.segments == 2 && step >= steps;
+        const int64_t k0 = int64_t(step - segment * steps) * kStep<T>;
+        const int left = step < last ? int(p.k - k0) : 0, at = m0 + h * 128;
+        sa[h].load((segment ? p.a[1] : p.a[0]) + (AK ? at * int64_t(p.a_row) + k0 * EL : k0 * p.a_row + int64_t(at) * EL), p.a_row, p.m - at,
+                   left, to + (h ? kA1 : kA0), part);
+    };
+    auto load_b = [&](int h, int step, uint32_t to) {
+        const int segment = w.segments == 2 && step >= steps;
+        if (w.segments == 2 && step == steps) aim_b(h, 1);
+        const int64_t k0 = int64_t(step - segment * steps) * kStep<T>;
+        const uint32_t row = (EPI == kGated ? h : segment) ? p.b_row[1] : p.b_row[0];
+        const int left = step < last ? int(p.k - k0) : 0, at = n0 + (EPI == kGated ? 0 : h * 128);
+        const char *src = (EPI == kGated ? h : segment) ? p.b[1] : p.b[0];
+        sb[h].load(src + (BK ? at * int64_t(row) + k0 * EL : k0 * row + int64_t(at) * EL), row, p.n - at, left,
+                   to + (h ? kB1 : kB0), part);
+    };
+
+    typename PA::template Lanes<4> la;
+    typename PB::template Lanes<2> lb;
+    la.init(lane, base, wm * 64);
+    lb.init(lane, base, wn * 32);
+    f32x4_t acc[2][4][2][2] = {};
+    u32x4_t a[4][2], b0[2][2], b1[2][2], next[2][2];
+    auto read_a = [&](uint32_t at) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < NT; ++j) {
-                    const int n = n0 + h * (BN / 2) + wn * (BN / 4) + 16 * j + 4 * fk;
-                    if (n >= p.n) continue;
-                    const f32x4_t c = acc[i][h][j];
-                    if constexpr (EPI == kGatedGrad) {
-                        const int64_t at = m * w.hidden_s + n, to = int64_t(m) * p.n + n;
-                        const f32x4_t g = load4(static_cast<const T *>(w.gate) + at), u = load4(static_cast<const T *>(w.up) + at);
-                        f32x4_t dg, du;
+            for (int s = 0; s < 2; ++s) a[i][s] = la.frag(i, s, at);
+    };
+    auto read_b = [&](u32x4_t(&b)[2][2], uint32_t at) {
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float slope;
-                            du[e] = c[e] * activation(w.gelu, g[e], &slope);
-                            dg[e] = c[e] * u[e] * slope;
-                        }
-                        store4(static_cast<T *>(p.c) + to, dg);
-                        store4(static_cast<T *>(p.c) + int64_t(p.m) * p.n + to, du);
-                    } else if (w.slices > 1) {
-                        store4(w.partial + slice * w.slice_size + p.partial + int64_t(m) * p.n + n, c);
-                    } else {
-                        store4(static_cast<T *>(p.c) + m * p.c_row + n, c);
-                    }
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) b[j][s] = lb.frag(j, s, at);
+    };
+    // the phase's reads have returned, and the next phase's panel has landed
+    auto meet_read = [&]() {
+        asm volatile("s_waitcnt vmcnt(12) lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(1);
+    };
+    auto meet = [&]() {
+        __builtin_amdgcn_s_setprio(0);
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto multiply = [&](f32x4_t(&c)[4][2][2], int h, const u32x4_t(&b)[2][2]) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) c[i][h][j] = mma(T(), b[j][s], a[i][s], c[i][h][j]);
+    };
+
+    const int segment = first >= steps;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        sa[h].init(threadIdx.x, p.a_row, int64_t(p.m - m0 - h * 128) * EL);
+        aim_b(h, segment);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+        load_b(0, first + t, base + t * kStage);
+        load_a(0, first + t, base + t * kStage);
+        load_b(1, first + t, base + t * kStage);
+        load_a(1, first + t, base + t * kStage);
+    }
+    asm volatile("s_waitcnt vmcnt(12)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    read_b(b0, kB0);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    if (wave >= 4) __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    for (int step = first; step < last; ++step) {
+        const uint32_t at = ((step - first) & 1) * kStage, to = base + at;
+        read_a(at + kA0);
+        load_b(0, step + 2, to);
+        meet_read();
+        multiply(acc[0], 0, b0);
+        meet();
+        read_b(b1, at + kB1);
+        load_a(0, step + 2, to);
+        meet_read();
+        multiply(acc[0], 1, b1);
+        meet();
+        read_a(at + kA1);
+        load_b(1, step + 2, to);
+        meet_read();
+        multiply(acc[1], 1, b1);
+        meet();
+        read_b(next, (kStage - at) + kB0);
+        load_a(1, step + 2, to);
+        meet_read();
+        multiply(acc[1], 0, b0);
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) b0[j][s] = next[j][s];
+        meet();
+    }
+    if (wave < 4) __builtin_amdgcn_s_barrier();
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load into LDS outlives the block
+
+    const int fr = lane & 15, fk = lane >> 4;
+#pragma unroll
+    for (int g = 0; g < 2; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int m = m0 + g * 128 + wm * 64 + 16 * i + fr;
+            if (m >= p.m) continue;
+#pragma unroll
+            for (int h = 0; h < (EPI == kGated ? 1 : 2); ++h)
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int n = n0 + h * 128 + wn * 32 + 16 * j + 4 * fk;
+                    if (n < p.n) finish<T, EPI>(w, p, slice, m, n, acc[g][i][h][j], acc[g][i][1][j]);
                 }
         }
-    }
 }
 
 // Adds up the slices in their order and rounds.
@@ -262,7 +454,8 @@ Plan plan(const Size *sizes, int count, bool bf16, int64_t k, int segments, Epil
         for (int i = 0; i < count; ++i) n += tiles_of(sizes[i], b, epi == kGated ? b / 2 : b);
         return n;
     };
-    if (tiles(128) < cus) p.bm = p.bn = 64;
+    if (bf16 && tiles(256) >= cus) p.bm = p.bn = 256;
+    else if (tiles(128) < cus) p.bm = p.bn = 64;
     if (epi == kPlain) {
         const int64_t n = tiles(p.bm);
         // slices of four steps at least, until two blocks a CU
@@ -294,8 +487,10 @@ hipError_t launch(Work &w, const Plan &plan, float *partial, hipStream_t s) {
         w.slice_size += int64_t(p.m) * p.n;
         blocks += int64_t(p.tiles) * plan.slices;
     }
-    const Fold f = fold(blocks, 256);
-    if (plan.bm == 128) k_product<T, AK, BK, EPI, 128, 128><<<dim3(f.x, 1, f.z), 256, 0, s>>>(w);
+    const Fold f = fold(blocks, 512);
+    if (plan.bm == 256) {
+        if constexpr (sizeof(T) == 2) k_product_large<AK, BK, EPI><<<dim3(f.x, 1, f.z), 512, 0, s>>>(w);
+    } else if (plan.bm == 128) k_product<T, AK, BK, EPI, 128, 128><<<dim3(f.x, 1, f.z), 256, 0, s>>>(w);
     else k_product<T, AK, BK, EPI, 64, 64><<<dim3(f.x, 1, f.z), 256, 0, s>>>(w);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || plan.slices == 1) return e;

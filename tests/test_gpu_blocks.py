@@ -379,6 +379,8 @@ UNIT = [
     (1, 8, 8), (1, 384, 1536), (2, 72, 40), (5, 1032, 264), (16, 64, 64), (17, 328, 1000), (33, 2056, 136), (63, 128, 2056),
     (64, 256, 512), (65, 264, 520), (128, 128, 128), (129, 136, 264), (200, 24, 1104), (300, 512, 72), (1000, 200, 328),
     (2100, 40, 2056), (4200, 1032, 24), (5000, 16, 16), (35, 1032, 2056),
+    # the largest tiles: of the hidden layer, of the rows, of the weights
+    (4200, 328, 2056), (8400, 2056, 264), (600, 2056, 4104),
 ]
 
 
