@@ -75,7 +75,7 @@ struct Product {
 constexpr int kMaxProducts = 3;
 struct Work {
     Product p[kMaxProducts];
-    int32_t products, segments;
+    int32_t products;
     int32_t slices, per_slice;  // of the contracted axis, and steps of each
     float *partial;             // [slices][slice_size]
     int64_t slice_size;
@@ -91,11 +91,10 @@ enum Epilogue { kPlain, kGated, kGatedGrad };
 // take tiles that follow each other, in bands of kBand tiles of rows, so that their
 // operands meet in its L2.
 struct Spot {
-    int which, slice, tile_m, tile_n;  // which < 0: none, of a folded launch's last blocks
+    int which, slice, tile_m, tile_n;  // which < 0: none, past the last one
 };
 constexpr int kBand = 4;
-__device__ inline Spot spot(const Work &w) {
-    uint32_t id = blockIdx.z * gridDim.x + blockIdx.x;
+__device__ inline Spot spot(const Work &w, uint32_t id) {
     int which = 0;
     uint32_t tiles = w.p[0].tiles, across = w.p[0].tiles_n;
 #pragma unroll
@@ -118,86 +117,100 @@ __device__ inline Spot spot(const Work &w) {
 // A copy by constant indexes: an indexed one would go through memory.
 __device__ inline Product pick(const Work &w, int which) { return which == 0 ? w.p[0] : which == 1 ? w.p[1] : w.p[2]; }
 
-// Stores four neighbouring results c (a gated product's: of gate, with those of up
+// Stores eight neighbouring results c (a gated product's: of gate, with those of up
 // in d) of row m from column n on.
 template <typename T, int EPI>
-__device__ inline void finish(const Work &w, const Product &p, int slice, int m, int n, f32x4_t c, f32x4_t d) {
+__device__ inline void finish(const Work &w, const Product &p, int slice, int m, int n, const float *c, const float *d) {
+    if (m >= p.m || n >= p.n) return;
     if constexpr (EPI == kGated) {
         const int64_t at = m * w.hidden_s + n;
-        f32x4_t h;
+        float h[8];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) h[e] = activation(w.gelu, c[e], nullptr) * d[e];
-        store4(static_cast<T *>(w.act) + at, h);
+        for (int e = 0; e < 8; ++e) h[e] = activation(w.gelu, c[e], nullptr) * d[e];
+        store8(static_cast<T *>(w.act) + at, h);
         if (w.gate) {
-            store4(static_cast<T *>(w.gate) + at, c);
-            store4(static_cast<T *>(w.up) + at, d);
+            store8(static_cast<T *>(w.gate) + at, c);
+            store8(static_cast<T *>(w.up) + at, d);
         }
     } else if constexpr (EPI == kGatedGrad) {
         const int64_t at = m * w.hidden_s + n, to = int64_t(m) * p.n + n;
-        const f32x4_t g = load4(static_cast<const T *>(w.gate) + at), u = load4(static_cast<const T *>(w.up) + at);
-        f32x4_t dg, du;
+        float g[8], u[8], dg[8], du[8];
+        load8(static_cast<const T *>(w.gate) + at, g);
+        load8(static_cast<const T *>(w.up) + at, u);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < 8; ++e) {
             float slope;
             du[e] = c[e] * activation(w.gelu, g[e], &slope);
             dg[e] = c[e] * u[e] * slope;
         }
-        store4(static_cast<T *>(p.c) + to, dg);
-        store4(static_cast<T *>(p.c) + int64_t(p.m) * p.n + to, du);
+        store8(static_cast<T *>(p.c) + to, dg);
+        store8(static_cast<T *>(p.c) + int64_t(p.m) * p.n + to, du);
     } else if (w.slices > 1) {
-        store4(w.partial + slice * w.slice_size + p.partial + int64_t(m) * p.n + n, c);
+        store8(w.partial + slice * w.slice_size + p.partial + int64_t(m) * p.n + n, c);
     } else {
-        store4(static_cast<T *>(p.c) + m * p.c_row + n, c);
+        store8(static_cast<T *>(p.c) + m * p.c_row + n, c);
     }
 }
 
 // Columns of a tile lie in two halves of BN / 2 (of a gated product: of gate and
-// up).  Four waves, two by two.
-template <typename T, bool AK, bool BK, int EPI, int BM, int BN>
-__global__ __launch_bounds__(256) void k_product(Work w) {
-    constexpr int EL = sizeof(T), MT = BM / 32, NT = BN / 64;
+// up).  Four waves, two by two.  STAGES buffers form a ring: the loads run STAGES - 1
+// steps ahead.  A step has two halves, whose fragments have registers of their own:
+// one half's are read while the other's are multiplied.  Reads and loads stand
+// between the products, so that one wave on a SIMD keeps all units busy.
+template <typename T, bool AK, bool BK, int EPI, int BM, int BN, int STAGES>
+__global__ __launch_bounds__(256, 2) void k_product(Work w) {
+    constexpr int MT = BM / 32, NT = BN / 64;
+    constexpr bool kGate = EPI == kGated, kTwo = EPI == kPlain && AK && !BK;  // kTwo: two segments
     typedef Panel<T, AK, BM> PA;
     typedef Panel<T, BK, BN / 2> PB;
+    typedef typename PA::template Feed<256> FA;
+    typedef typename PB::template Feed<256> FB;
     constexpr uint32_t kStage = PA::kBytes + 2 * PB::kBytes;
-    __shared__ __attribute__((aligned(1024))) char lds[2 * kStage];
+    constexpr int kLoads = FA::kLoads + 2 * FB::kLoads, kStep = PA::kStep;
+    __shared__ __attribute__((aligned(1024))) char lds[STAGES * kStage];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave >> 1, wn = wave & 1;
-    const Spot at_tile = spot(w);
-    if (at_tile.which < 0) return;
-    const Product p = pick(w, at_tile.which);
-    const int slice = at_tile.slice;
-    const int m0 = at_tile.tile_m * BM, n0 = at_tile.tile_n * (EPI == kGated ? BN / 2 : BN);
-    const int steps = (p.k + kStep<T> - 1) / kStep<T>;
-    const int first = slice * w.per_slice, last = min(first + w.per_slice, steps * w.segments);
+    const Spot tile = spot(w, blockIdx.z * gridDim.x + blockIdx.x);
+    if (tile.which < 0) return;
+    const Product p = pick(w, tile.which);
+    const int m0 = tile.tile_m * BM, n0 = tile.tile_n * (kGate ? BN / 2 : BN);
+    const int steps = (p.k + kStep - 1) / kStep;  // of a segment
+    const int first = tile.slice * w.per_slice, last = min(first + w.per_slice, steps * (kTwo ? 2 : 1));
 
-    const uint32_t base = lds_offset(lds), part = uint32_t(wave) * 1024u;
-    typename PA::template Stager<256> sa;
-    typename PB::template Stager<256> sb[2];
-    int segment = first >= steps;
-    auto aim = [&]() {
-        sa.init(threadIdx.x, p.a_row, int64_t(p.m - m0) * EL);
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-            sb[h].init(threadIdx.x, (EPI == kGated ? h : segment) ? p.b_row[1] : p.b_row[0], int64_t(p.n - n0 - (EPI == kGated ? 0 : h * (BN / 2))) * EL);
-    };
-    auto load = [&](int step, uint32_t to) {
-        if (w.segments == 2 && segment == 0 && step >= steps) {
-            segment = 1;
-            aim();
-        }
-        const int64_t k0 = int64_t(step - segment * steps) * kStep<T>;
-        const int left = int(p.k - k0);
-        sa.load((segment ? p.a[1] : p.a[0]) + (AK ? m0 * int64_t(p.a_row) + k0 * EL : k0 * p.a_row + int64_t(m0) * EL), p.a_row, p.m - m0,
-                left, to, part);
+    FA fa;
+    FB fb[2];
+    Steps walk;
+    int switch_in = 0;  // steps before the second segment
+    auto aim = [&](int segment, int step) {
+        fa.init(threadIdx.x, segment ? p.a[1] : p.a[0], p.a_row, m0, p.m - m0, step);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const uint32_t row = (EPI == kGated ? h : segment) ? p.b_row[1] : p.b_row[0];
-            const int at = n0 + (EPI == kGated ? 0 : h * (BN / 2));
-            const char *src = (EPI == kGated ? h : segment) ? p.b[1] : p.b[0];
-            sb[h].load(src + (BK ? at * int64_t(row) + k0 * EL : k0 * row + int64_t(at) * EL), row, p.n - at, left,
-                       to + PA::kBytes + h * PB::kBytes, part);
+            const int at = n0 + (kGate ? 0 : h * (BN / 2)), from = kGate ? h : segment;
+            fb[h].init(threadIdx.x, from ? p.b[1] : p.b[0], from ? p.b_row[1] : p.b_row[0], at, p.n - at, step);
         }
+        walk.left = p.k - step * kStep;
+    };
+    const int segment = kTwo && first >= steps;
+    aim(segment, first - segment * steps);
+    walk.more = last - first;
+    if (kTwo) switch_in = segment ? -1 : steps - first;
+
+    // A step's loads, one at a time.
+    const uint32_t base = lds_offset(lds), part = uint32_t(wave) * 1024u;
+    u32x4_t ra, rb[2];
+    int k = 0;
+    auto prepare = [&]() {
+        if (kTwo && switch_in-- == 0) aim(1, 0);
+        k = walk.next<kStep>();
+        ra = fa.next(k);
+        rb[0] = fb[0].next(k);
+        rb[1] = fb[1].next(k);
+    };
+    auto load = [&](int n, uint32_t to) {
+        if (n < FA::kLoads) fa.load(n, ra, k, to + part);
+        else if (n < FA::kLoads + FB::kLoads) fb[0].load(n - FA::kLoads, rb[0], k, to + PA::kBytes + part);
+        else fb[1].load(n - FA::kLoads - FB::kLoads, rb[1], k, to + PA::kBytes + PB::kBytes + part);
     };
 
     typename PA::template Lanes<MT> la;
@@ -205,115 +218,147 @@ __global__ __launch_bounds__(256) void k_product(Work w) {
     la.init(lane, base, wm * (BM / 2));
     lb.init(lane, base + PA::kBytes, wn * (BN / 4));
     f32x4_t acc[MT][2][NT] = {};
-    aim();
-    if (first < last) load(first, base);
-    for (int step = first; step < last; ++step) {
-        // this step's tiles are there, and the other buffer is free
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        asm volatile("" ::: "memory");
-        const uint32_t at = ((step - first) & 1) * kStage;
-        if (step + 1 < last) load(step + 1, base + (kStage - at));
+    u32x4_t a[2][MT], b[2][2][NT];
+    constexpr int kReads = MT + 2 * NT;
+    auto read = [&](int n, int s, uint32_t at) {
+        if (n < MT) a[s][n] = la.frag(n, s, at);
+        else b[s][(n - MT) / NT][(n - MT) % NT] = lb.frag((n - MT) % NT, s, at + (n - MT) / NT * PB::kBytes);
+    };
+    // The products of half s, with `items` calls of item spread between them.
+    auto multiply = [&](int s, int items, auto item) {
+        constexpr int kAll = MT * 2 * NT * kMmaSteps<T>;
+        int done = 0;
 #pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            u32x4_t fa[MT], fb[2][NT];
-#pragma unroll
-            for (int i = 0; i < MT; ++i) fa[i] = la.frag(i, s, at);
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) fb[h][j] = lb.frag(j, s, at + h * PB::kBytes);
+        for (int e = 0; e < kMmaSteps<T>; ++e)
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int j = 0; j < NT; ++j) acc[i][h][j] = mma(T(), fb[h][j], fa[i], acc[i][h][j]);
-        }
+                    for (int j = 0; j < NT; ++j) {
+                        const int q = ((e * MT + i) * 2 + h) * NT + j;
+                        acc[i][h][j] = mma(T(), e, b[s][h][j], a[s][i], acc[i][h][j]);
+#pragma unroll
+                        for (; done < (q + 1) * items / kAll; ++done) item(done);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+    };
+    // the next step's panels have landed and this wave's reads have returned: so
+    // they have for all waves
+    auto meet = [&]() {
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((STAGES - 2) * kLoads) : "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+#pragma unroll
+    for (int t = 0; t < STAGES; ++t) {
+        if (t == STAGES - 1) meet();
+        prepare();
+#pragma unroll
+        for (int n = 0; n < kLoads; ++n) load(n, base + t * kStage);
     }
+#pragma unroll
+    for (int n = 0; n < kReads; ++n) read(n, 0, 0);
+    uint32_t at = 0;
+    for (int step = first; step < last; ++step) {
+        const uint32_t then = at + kStage == STAGES * kStage ? 0 : at + kStage;
+        multiply(0, kReads + 1, [&](int n) {
+            if (n < kReads) read(n, 1, at);
+            else prepare();
+        });
+        meet();
+        multiply(1, kReads + kLoads, [&](int n) {
+            if (n < kReads) read(n, 0, then);
+            else load(n - kReads, base + at);
+        });
+        at = then;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load into LDS outlives the block
 
-    const int fr = lane & 15, fk = lane >> 4;
+    // pairs of tiles side by side, or below each other where there is one
+    constexpr int kDown = NT == 1 ? 2 : 1;
+    static_assert(NT * kDown == 2, "pairs");
+    const int fr = lane & 15, second = (lane >> 4) & 1, col = (lane >> 5) * 8;
 #pragma unroll
-    for (int i = 0; i < MT; ++i) {
-        const int m = m0 + wm * (BM / 2) + 16 * i + fr;
-        if (m >= p.m) continue;
+    for (int i = 0; i < MT; i += kDown)
 #pragma unroll
-        for (int h = 0; h < (EPI == kGated ? 1 : 2); ++h)
-#pragma unroll
-            for (int j = 0; j < NT; ++j) {
-                const int n = n0 + h * (BN / 2) + wn * (BN / 4) + 16 * j + 4 * fk;
-                if (n < p.n) finish<T, EPI>(w, p, slice, m, n, acc[i][h][j], acc[i][1][j]);
-            }
-    }
+        for (int h = 0; h < (kGate ? 1 : 2); ++h) {
+            float c[8], d[8];
+            pair_up(acc[i][h][0], acc[i + kDown - 1][h][NT - 1], c);
+            if (kGate) pair_up(acc[i][1][0], acc[i + kDown - 1][1][NT - 1], d);
+            finish<T, EPI>(w, p, tile.slice, m0 + wm * (BM / 2) + 16 * (i + (kDown - 1) * second) + fr,
+                           n0 + h * (BN / 2) + wn * (BN / 4) + 16 * (NT - 1) * second + col, c, d);
+        }
 }
 
 // bf16, tiles of 256 x 256, eight waves of 128 x 64: rows 64 wm .. of both halves of
 // the tile's rows, columns 32 wn .. of both halves of its columns.  A step's four
 // panels (two halves of A, two of B) have two buffers.  A wave goes through a step in
 // four phases, each a quarter of its results:
-//   1: reads A0             products of A0, B0     (B0 is in registers)
-//   2: reads B1             products of A0, B1
-//   3: reads A1             products of A1, B1
-//   4: reads the next B0    products of A1, B0
+//   1: reads A0, B0    products of A0, B0
+//   2: reads B1        products of A0, B1
+//   3: reads A1        products of A1, B1
+//   4:                 products of A1, B0
 // A phase reads, waits, meets the other waves at a barrier, multiplies, and meets
 // them again.  Waves 4 .. 7 (the second wave of every SIMD) run one barrier behind,
 // so that on each SIMD one wave multiplies while the other reads.  A panel that
-// phase p has read is free in phase p + 1 and filled there with its values of two
-// steps later; loads are waited for one phase before they are read, with those of
-// the last six panels still under way.
+// phase p has read is free in phase p + 1; phases 2, 3, 4 and the next 1 fill B0, A0,
+// B1 and A1 with their values of two steps later (in this order all along).  Loads are
+// waited for one phase before they are read, with those of the last five panels
+// still under way.  Blocks stay and take every gridDim.x-th tile;
+// the next tile's first loads are under way while this one's results are stored.
 template <bool AK, bool BK, int EPI>
 __global__ __launch_bounds__(512) void k_product_large(Work w) {
     typedef uint16_t T;
-    constexpr int EL = 2, BM = 256, BN = 256;
+    constexpr int BM = 256, BN = 256;
+    constexpr bool kGate = EPI == kGated, kTwo = EPI == kPlain && AK && !BK;  // kTwo: two segments
     typedef Panel<T, AK, 128> PA;
     typedef Panel<T, BK, 128> PB;
+    constexpr int kStep = PA::kStep;
     constexpr uint32_t kPanel = 128 * 128, kStage = 4 * kPanel;
     constexpr uint32_t kA0 = 0, kA1 = kPanel, kB0 = 2 * kPanel, kB1 = 3 * kPanel;
     __shared__ __attribute__((aligned(1024))) char lds[2 * kStage];
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave >> 2, wn = wave & 3;
-    const Spot at_tile = spot(w);
-    if (at_tile.which < 0) return;
-    const Product p = pick(w, at_tile.which);
-    const int slice = at_tile.slice;
-    const int m0 = at_tile.tile_m * BM, n0 = at_tile.tile_n * (EPI == kGated ? BN / 2 : BN);
-    const int steps = (p.k + kStep<T> - 1) / kStep<T>;
-    const int first = slice * w.per_slice, last = min(first + w.per_slice, steps * w.segments);
-
     const uint32_t base = lds_offset(lds), part = uint32_t(wave) * 1024u;
-    typename PA::template Stager<512> sa[2];
-    typename PB::template Stager<512> sb[2];
-    static_assert(sa[0].kLoads == 2 && sb[0].kLoads == 2, "the waits count two loads a panel");
-    auto aim_b = [&](int h, int segment) {
-        sb[h].init(threadIdx.x, (EPI == kGated ? h : segment) ? p.b_row[1] : p.b_row[0], int64_t(p.n - n0 - (EPI == kGated ? 0 : h * 128)) * EL);
-    };
-    // The panels of half h in the buffer `to`; past the slice's end nothing is
+    typename PA::template Feed<512> fa[2];
+    typename PB::template Feed<512> fb[2];
+    static_assert(fa[0].kLoads == 2 && fb[0].kLoads == 2, "the waits count two loads a panel");
+    Steps walk;
+    int switch_in = 0, k = 0;  // steps before the second segment; values of the step that is loaded
+    Spot tile = {};
+    Product p = w.p[0];
+    int m0 = 0, n0 = 0, steps = 0, count = 0;  // of the tile; steps of a segment, and of the slice
+    // The four loads of a step, in this order; past the slice's end nothing is
     // fetched and zeros are stored, so that the number of loads stays the same.
-    auto load_a = [&](int h, int step, uint32_t to) {
-        const int segment = w.segments == 2 && step >= steps;
-        const int64_t k0 = int64_t(step - segment * steps) * kStep<T>;
-        const int left = step < last ? int(p.k - k0) : 0, at = m0 + h * 128;
-        sa[h].load((segment ? p.a[1] : p.a[0]) + (AK ? at * int64_t(p.a_row) + k0 * EL : k0 * p.a_row + int64_t(at) * EL), p.a_row, p.m - at,
-                   left, to + (h ? kA1 : kA0), part);
+    auto load_a = [&](int h, uint32_t to) {
+        const u32x4_t r = fa[h].next(k);
+        fa[h].load(0, r, k, to + (h ? kA1 : kA0) + part);
+        fa[h].load(1, r, k, to + (h ? kA1 : kA0) + part);
     };
-    auto load_b = [&](int h, int step, uint32_t to) {
-        const int segment = w.segments == 2 && step >= steps;
-        if (w.segments == 2 && step == steps) aim_b(h, 1);
-        const int64_t k0 = int64_t(step - segment * steps) * kStep<T>;
-        const uint32_t row = (EPI == kGated ? h : segment) ? p.b_row[1] : p.b_row[0];
-        const int left = step < last ? int(p.k - k0) : 0, at = n0 + (EPI == kGated ? 0 : h * 128);
-        const char *src = (EPI == kGated ? h : segment) ? p.b[1] : p.b[0];
-        sb[h].load(src + (BK ? at * int64_t(row) + k0 * EL : k0 * row + int64_t(at) * EL), row, p.n - at, left,
-                   to + (h ? kB1 : kB0), part);
+    auto load_b = [&](int h, uint32_t to) {
+        if (h == 0) {
+            if (kTwo && switch_in-- == 0) {
+                // the segments' rows are equally far apart: only the bases differ
+                const uint64_t da = p.a[1] - p.a[0] - steps * int64_t(fa[0].ahead);
+                const uint64_t db = p.b[1] - p.b[0] - steps * int64_t(fb[0].ahead);
+                fa[0].at += da, fa[1].at += da, fb[0].at += db, fb[1].at += db;
+                walk.left = p.k;
+            }
+            k = walk.next<kStep>();
+        }
+        const u32x4_t r = fb[h].next(k);
+        fb[h].load(0, r, k, to + (h ? kB1 : kB0) + part);
+        fb[h].load(1, r, k, to + (h ? kB1 : kB0) + part);
     };
-
     typename PA::template Lanes<4> la;
     typename PB::template Lanes<2> lb;
     la.init(lane, base, wm * 64);
     lb.init(lane, base, wn * 32);
     f32x4_t acc[2][4][2][2] = {};
-    u32x4_t a[4][2], b0[2][2], b1[2][2], next[2][2];
+    u32x4_t a[4][2], b0[2][2], b1[2][2];
     auto read_a = [&](uint32_t at) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -328,7 +373,7 @@ __global__ __launch_bounds__(512) void k_product_large(Work w) {
     };
     // the phase's reads have returned, and the next phase's panel has landed
     auto meet_read = [&]() {
-        asm volatile("s_waitcnt vmcnt(12) lgkmcnt(0)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(10) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
@@ -346,123 +391,150 @@ __global__ __launch_bounds__(512) void k_product_large(Work w) {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) c[i][h][j] = mma(T(), b[j][s], a[i][s], c[i][h][j]);
+                for (int j = 0; j < 2; ++j) c[i][h][j] = mma(T(), 0, b[j][s], a[i][s], c[i][h][j]);
     };
 
-    const int segment = first >= steps;
+    for (uint32_t id = blockIdx.x;; id += gridDim.x) {
+        // All waves are done with the buffers: the next tile's first loads go ahead
+        // of the stores of the one before.
+        const Product before = p;
+        const int slice = tile.slice, row = m0 + wm * 64 + (lane & 15);
+        const int col = n0 + wn * 32 + 16 * ((lane >> 4) & 1) + (lane >> 5) * 8;
+        tile = spot(w, id);
+        if (tile.which >= 0) {
+            p = pick(w, tile.which);
+            m0 = tile.tile_m * BM, n0 = tile.tile_n * (kGate ? BN / 2 : BN);
+            steps = (p.k + kStep - 1) / kStep;
+            const int first = tile.slice * w.per_slice;
+            const int segment = kTwo && first >= steps, step = first - segment * steps;
+            count = min(w.per_slice, steps * (kTwo ? 2 : 1) - first);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        sa[h].init(threadIdx.x, p.a_row, int64_t(p.m - m0 - h * 128) * EL);
-        aim_b(h, segment);
-    }
+            for (int h = 0; h < 2; ++h) {
+                const int am = m0 + h * 128, an = n0 + (kGate ? 0 : h * 128), from = kGate ? h : segment;
+                fa[h].init(threadIdx.x, segment ? p.a[1] : p.a[0], p.a_row, am, p.m - am, step);
+                fb[h].init(threadIdx.x, from ? p.b[1] : p.b[0], from ? p.b_row[1] : p.b_row[0], an, p.n - an, step);
+            }
+            walk = {p.k - step * kStep, count};
+            if (kTwo) switch_in = segment ? -1 : steps - first;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-        load_b(0, first + t, base + t * kStage);
-        load_a(0, first + t, base + t * kStage);
-        load_b(1, first + t, base + t * kStage);
-        load_a(1, first + t, base + t * kStage);
-    }
-    asm volatile("s_waitcnt vmcnt(12)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    asm volatile("" ::: "memory");
-    read_b(b0, kB0);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    __builtin_amdgcn_s_barrier();
-    if (wave >= 4) __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_sched_barrier(0);
-    for (int step = first; step < last; ++step) {
-        const uint32_t at = ((step - first) & 1) * kStage, to = base + at;
-        read_a(at + kA0);
-        load_b(0, step + 2, to);
-        meet_read();
-        multiply(acc[0], 0, b0);
-        meet();
-        read_b(b1, at + kB1);
-        load_a(0, step + 2, to);
-        meet_read();
-        multiply(acc[0], 1, b1);
-        meet();
-        read_a(at + kA1);
-        load_b(1, step + 2, to);
-        meet_read();
-        multiply(acc[1], 1, b1);
-        meet();
-        read_b(next, (kStage - at) + kB0);
-        load_a(1, step + 2, to);
-        meet_read();
-        multiply(acc[1], 0, b0);
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int s = 0; s < 2; ++s) b0[j][s] = next[j][s];
-        meet();
-    }
-    if (wave < 4) __builtin_amdgcn_s_barrier();
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load into LDS outlives the block
-
-    const int fr = lane & 15, fk = lane >> 4;
-#pragma unroll
-    for (int g = 0; g < 2; ++g)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int m = m0 + g * 128 + wm * 64 + 16 * i + fr;
-            if (m >= p.m) continue;
-#pragma unroll
-            for (int h = 0; h < (EPI == kGated ? 1 : 2); ++h)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int n = n0 + h * 128 + wn * 32 + 16 * j + 4 * fk;
-                    if (n < p.n) finish<T, EPI>(w, p, slice, m, n, acc[g][i][h][j], acc[g][i][1][j]);
-                }
+            for (int t = 0; t < 2; ++t) {
+                load_b(0, base + t * kStage);
+                load_a(0, base + t * kStage);
+                load_b(1, base + t * kStage);
+                if (t == 0) load_a(1, base);
+            }
         }
+        if (id != blockIdx.x) {
+#pragma unroll
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int h = 0; h < (kGate ? 1 : 2); ++h) {
+                        float c[8], d[8];
+                        pair_up(acc[g][i][h][0], acc[g][i][h][1], c);
+                        if (kGate) pair_up(acc[g][i][1][0], acc[g][i][1][1], d);
+                        finish<T, EPI>(w, before, slice, row + g * 128 + 16 * i, col + h * 128, c, d);
+                    }
+        }
+        if (tile.which < 0) break;
+        // the first two panels (and all but the last stores of the tile before)
+        asm volatile("s_waitcnt vmcnt(10)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        if (wave >= 4) __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) acc[i / 16][i / 4 % 4][i / 2 % 2][i % 2] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        uint32_t at = 0;
+        for (int step = 0; step < count; ++step) {
+            const uint32_t to = base + at;
+            read_a(at + kA0);
+            read_b(b0, at + kB0);
+            load_a(1, base + (kStage - at));
+            meet_read();
+            multiply(acc[0], 0, b0);
+            meet();
+            read_b(b1, at + kB1);
+            load_b(0, to);
+            meet_read();
+            multiply(acc[0], 1, b1);
+            meet();
+            read_a(at + kA1);
+            load_a(0, to);
+            meet_read();
+            multiply(acc[1], 1, b1);
+            meet();
+            load_b(1, to);
+            meet_read();
+            multiply(acc[1], 0, b0);
+            meet();
+            at = kStage - at;
+        }
+        if (wave < 4) __builtin_amdgcn_s_barrier();
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // this wave's loads of zeros past the last step
+    }
 }
 
 // Adds up the slices in their order and rounds.
 template <typename T>
 __global__ __launch_bounds__(256) void k_join_slices(Work w) {
-    for (int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 4; i < w.slice_size; i += int64_t(gridDim.x) * 1024) {
+    for (int64_t i = (int64_t(blockIdx.x) * 256 + threadIdx.x) * 8; i < w.slice_size; i += int64_t(gridDim.x) * 2048) {
         int which = 0;
         while (which + 1 < w.products && i >= w.p[which + 1].partial) ++which;
         const Product &p = w.p[which];
-        f32x4_t sum = load4(w.partial + i);
-        for (int s = 1; s < w.slices; ++s) sum += load4(w.partial + s * w.slice_size + i);
+        float sum[8], more[8];
+        load8(w.partial + i, sum);
+        for (int s = 1; s < w.slices; ++s) {
+            load8(w.partial + s * w.slice_size + i, more);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[e] += more[e];
+        }
         const int64_t at = i - p.partial, m = at / p.n;
-        store4(static_cast<T *>(p.c) + m * p.c_row + (at - m * p.n), sum);
+        store8(static_cast<T *>(p.c) + m * p.c_row + (at - m * p.n), sum);
     }
 }
 
 // ------------------------------------------------------------------------ plan
 
-// Tile sizes and slices of a launch of products with one contracted length.
+// Tiles and slices of a launch of products with one contracted length.
+enum Tiles { kTiles256, kTiles128, kTiles64 };
 struct Plan {
-    int bm, bn, slices, per_slice, steps;
+    Tiles kind;
+    int slices, per_slice, steps;
     size_t partial;  // bytes
 };
-
+constexpr int kRowsOf[] = {256, 128, 64}, kColsOf[] = {256, 128, 64};
 struct Size {
     int64_t m, n;
 };
 
-// cols: columns of a result that a tile of bn holds: bn, or half of a gated one.
-int64_t tiles_of(const Size &s, int bm, int cols) { return ((s.m + bm - 1) / bm) * ((s.n + cols - 1) / cols); }
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+// Columns of a result that a tile holds.
+int cols_of(Tiles kind, Epilogue epi) { return epi == kGated ? kColsOf[kind] / 2 : kColsOf[kind]; }
+int64_t tiles_of(const Size &s, Tiles kind, Epilogue epi) {
+    return ceil_div(s.m, kRowsOf[kind]) * ceil_div(s.n, cols_of(kind, epi));
+}
 
-Plan plan(const Size *sizes, int count, bool bf16, int64_t k, int segments, Epilogue epi) {
-    const int cus = compute_units(), step = bf16 ? 64 : 32;
-    Plan p{128, 128, 1, 0, int((k + step - 1) / step) * segments, 0};
-    auto tiles = [&](int b) {
+// large: whether the largest tiles may be taken.
+Plan plan(const Size *sizes, int count, bool bf16, int64_t k, int segments, Epilogue epi, bool large = true) {
+    const int cus = compute_units(), elem = bf16 ? 2 : 4;
+    Plan p{};
+    auto tiles = [&](Tiles kind) {
         int64_t n = 0;
-        for (int i = 0; i < count; ++i) n += tiles_of(sizes[i], b, epi == kGated ? b / 2 : b);
+        for (int i = 0; i < count; ++i) n += tiles_of(sizes[i], kind, epi);
         return n;
     };
-    if (bf16 && tiles(256) >= cus) p.bm = p.bn = 256;
-    else if (tiles(128) < cus) p.bm = p.bn = 64;
+    p.kind = bf16 && large && tiles(kTiles256) >= cus ? kTiles256 : tiles(kTiles128) >= cus ? kTiles128 : kTiles64;
+    p.slices = 1;
+    p.steps = int(ceil_div(k, 128 / elem)) * segments;
     if (epi == kPlain) {
-        const int64_t n = tiles(p.bm);
+        const int64_t n = tiles(p.kind);
         // slices of four steps at least, until two blocks a CU
         if (n < cus) p.slices = int(std::max<int64_t>(1, std::min<int64_t>(p.steps / 4, 2 * cus / std::max<int64_t>(n, 1))));
     }
-    p.per_slice = (p.steps + p.slices - 1) / p.slices;
-    p.slices = p.per_slice ? (p.steps + p.per_slice - 1) / p.per_slice : 1;
+    p.per_slice = int(ceil_div(p.steps, p.slices));
+    p.slices = p.per_slice ? int(ceil_div(p.steps, p.per_slice)) : 1;
     if (p.slices > 1) {
         int64_t values = 0;
         for (int i = 0; i < count; ++i) values += sizes[i].m * sizes[i].n;
@@ -480,21 +552,24 @@ hipError_t launch(Work &w, const Plan &plan, float *partial, hipStream_t s) {
     w.slice_size = 0;
     for (int i = 0; i < w.products; ++i) {
         Product &p = w.p[i];
-        const int cols = EPI == kGated ? plan.bn / 2 : plan.bn;
-        p.tiles_n = (p.n + cols - 1) / cols;
-        p.tiles = int(tiles_of({p.m, p.n}, plan.bm, cols));
+        p.tiles_n = int(ceil_div(p.n, cols_of(plan.kind, Epilogue(EPI))));
+        p.tiles = int(tiles_of({p.m, p.n}, plan.kind, Epilogue(EPI)));
         p.partial = w.slice_size;
         w.slice_size += int64_t(p.m) * p.n;
         blocks += int64_t(p.tiles) * plan.slices;
     }
-    const Fold f = fold(blocks, 512);
-    if (plan.bm == 256) {
-        if constexpr (sizeof(T) == 2) k_product_large<AK, BK, EPI><<<dim3(f.x, 1, f.z), 512, 0, s>>>(w);
-    } else if (plan.bm == 128) k_product<T, AK, BK, EPI, 128, 128><<<dim3(f.x, 1, f.z), 256, 0, s>>>(w);
-    else k_product<T, AK, BK, EPI, 64, 64><<<dim3(f.x, 1, f.z), 256, 0, s>>>(w);
+    const Fold f = fold(blocks, 256);
+    const dim3 grid(f.x, 1, f.z);
+    switch (plan.kind) {
+        case kTiles256:
+            if constexpr (sizeof(T) == 2) k_product_large<AK, BK, EPI><<<int(std::min<int64_t>(blocks, compute_units())), 512, 0, s>>>(w);
+            break;
+        case kTiles128: k_product<T, AK, BK, EPI, 128, 128, 2><<<grid, 256, 0, s>>>(w); break;
+        case kTiles64: k_product<T, AK, BK, EPI, 64, 64, 2><<<grid, 256, 0, s>>>(w); break;
+    }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || plan.slices == 1) return e;
-    k_join_slices<T><<<int(std::min<int64_t>((w.slice_size + 1023) / 1024, 8 * compute_units())), 256, 0, s>>>(w);
+    k_join_slices<T><<<int(std::min<int64_t>((w.slice_size + 2047) / 2048, 8 * compute_units())), 256, 0, s>>>(w);
     return hipGetLastError();
 }
 
@@ -514,7 +589,7 @@ Plan plan_dhidden(const FfnArgs &a) {
 }
 Plan plan_dx(const FfnArgs &a) {
     const Size s{a.rows, a.channels};
-    return plan(&s, 1, a.bf16, a.hidden, 2, kPlain);
+    return plan(&s, 1, a.bf16, a.hidden, 2, kPlain, a.w_gate_s == a.w_up_s);
 }
 Plan plan_weights(const FfnArgs &a) {
     Size s[kMaxProducts];
@@ -538,7 +613,7 @@ hipError_t forward(FfnArgs a, hipStream_t s) {
         space += round16(hidden_bytes(a));
     }
     Work w{};
-    w.products = w.segments = 1;
+    w.products = 1;
     w.gelu = a.gelu;
     w.gate = a.gate, w.up = a.up, w.act = a.act, w.hidden_s = a.hidden_s;
     Product &p = w.p[0];
@@ -567,7 +642,7 @@ hipError_t gradient(const FfnArgs &a, hipStream_t s) {
     hipError_t e;
     if (a.rows > 0 && wants_hidden(a)) {
         Work w{};
-        w.products = w.segments = 1;
+        w.products = 1;
         w.gelu = a.gelu;
         w.gate = a.gate, w.up = a.up, w.hidden_s = a.hidden_s;
         Product &p = w.p[0];
@@ -579,7 +654,7 @@ hipError_t gradient(const FfnArgs &a, hipStream_t s) {
     }
     if (a.rows > 0 && a.dx) {
         Work w{};
-        w.products = 1, w.segments = 2;
+        w.products = 1;
         Product &p = w.p[0];
         p.a[0] = dgate, p.a[1] = dup;
         p.b[0] = static_cast<const char *>(a.w_gate), p.b[1] = static_cast<const char *>(a.w_up);
@@ -590,7 +665,6 @@ hipError_t gradient(const FfnArgs &a, hipStream_t s) {
         if ((e = launch<T, true, false, kPlain>(w, plan_dx(a), partial, s)) != hipSuccess) return e;
     }
     Work w{};
-    w.segments = 1;
     auto add = [&](void *c, int64_t c_row, const void *from, uint32_t from_row, const void *with, uint32_t with_row, int m, int n) {
         if (!c) return;
         Product &p = w.p[w.products++];
