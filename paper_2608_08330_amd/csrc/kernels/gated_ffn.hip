@@ -117,38 +117,75 @@ __device__ inline Spot spot(const Work &w, uint32_t id) {
 // A copy by constant indexes: an indexed one would go through memory.
 __device__ inline Product pick(const Work &w, int which) { return which == 0 ? w.p[0] : which == 1 ? w.p[1] : w.p[2]; }
 
-// Stores eight neighbouring results c (a gated product's: of gate, with those of up
-// in d) of row m from column n on.
-template <typename T, int EPI>
-__device__ inline void finish(const Work &w, const Product &p, int slice, int m, int n, const float *c, const float *d) {
-    if (m >= p.m || n >= p.n) return;
-    if constexpr (EPI == kGated) {
-        const int64_t at = m * w.hidden_s + n;
-        float h[8];
+// What a lane holds of a result: eight neighbouring columns of row m from column n on.
+struct Place {
+    int m, n;
+};
+
+// Stores a lane's UNITS results; at(u) is the place of the u-th, take(u, c, d) gives
+// its values c (a gated product's: of gate, with those of up in d).
+template <typename T, int EPI, int UNITS, class At, class Take>
+__device__ inline void finish(const Work &w, const Product &p, int slice, At at, Take take) {
+    if constexpr (EPI == kGatedGrad) {
+        // g and u a batch ahead: the loads are waited for together, from places
+        // that always exist
+        constexpr int kBatch = UNITS < 4 ? UNITS : 4, kBatches = UNITS / kBatch;
+        static_assert(UNITS % kBatch == 0, "whole batches");
+        float g[2][kBatch][8], u[2][kBatch][8];
+        auto fetch = [&](int b) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] = activation(w.gelu, c[e], nullptr) * d[e];
-        store8(static_cast<T *>(w.act) + at, h);
-        if (w.gate) {
-            store8(static_cast<T *>(w.gate) + at, c);
-            store8(static_cast<T *>(w.up) + at, d);
-        }
-    } else if constexpr (EPI == kGatedGrad) {
-        const int64_t at = m * w.hidden_s + n, to = int64_t(m) * p.n + n;
-        float g[8], u[8], dg[8], du[8];
-        load8(static_cast<const T *>(w.gate) + at, g);
-        load8(static_cast<const T *>(w.up) + at, u);
+            for (int i = 0; i < kBatch; ++i) {
+                const Place o = at(b * kBatch + i);
+                const int64_t from = min(o.m, p.m - 1) * w.hidden_s + min(o.n, p.n - 8);
+                load8(static_cast<const T *>(w.gate) + from, g[b & 1][i]);
+                load8(static_cast<const T *>(w.up) + from, u[b & 1][i]);
+            }
+        };
+        fetch(0);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            float slope;
-            du[e] = c[e] * activation(w.gelu, g[e], &slope);
-            dg[e] = c[e] * u[e] * slope;
+        for (int b = 0; b < kBatches; ++b) {
+            if (b + 1 < kBatches) fetch(b + 1);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const Place o = at(b * kBatch + i);
+                float c[8], dg[8], du[8];
+                take(b * kBatch + i, c, nullptr);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    float slope;
+                    du[e] = c[e] * activation(w.gelu, g[b & 1][i][e], &slope);
+                    dg[e] = c[e] * u[b & 1][i][e] * slope;
+                }
+                if (o.m >= p.m || o.n >= p.n) continue;
+                const int64_t to = int64_t(o.m) * p.n + o.n;
+                store8(static_cast<T *>(p.c) + to, dg);
+                store8(static_cast<T *>(p.c) + int64_t(p.m) * p.n + to, du);
+            }
         }
-        store8(static_cast<T *>(p.c) + to, dg);
-        store8(static_cast<T *>(p.c) + int64_t(p.m) * p.n + to, du);
-    } else if (w.slices > 1) {
-        store8(w.partial + slice * w.slice_size + p.partial + int64_t(m) * p.n + n, c);
     } else {
-        store8(static_cast<T *>(p.c) + m * p.c_row + n, c);
+#pragma unroll
+        for (int i = 0; i < UNITS; ++i) {
+            const Place o = at(i);
+            float c[8], d[8];
+            take(i, c, d);
+            if constexpr (EPI == kGated) {
+                float h[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) h[e] = activation(w.gelu, c[e], nullptr) * d[e];
+                if (o.m >= p.m || o.n >= p.n) continue;
+                const int64_t to = o.m * w.hidden_s + o.n;
+                store8(static_cast<T *>(w.act) + to, h);
+                if (w.gate) {
+                    store8(static_cast<T *>(w.gate) + to, c);
+                    store8(static_cast<T *>(w.up) + to, d);
+                }
+            } else {
+                if (o.m >= p.m || o.n >= p.n) continue;
+                if (w.slices > 1) store8(w.partial + slice * w.slice_size + p.partial + int64_t(o.m) * p.n + o.n, c);
+                else store8(static_cast<T *>(p.c) + o.m * p.c_row + o.n, c);
+            }
+        }
     }
 }
 
@@ -280,16 +317,17 @@ __global__ __launch_bounds__(256, 2) void k_product(Work w) {
     constexpr int kDown = NT == 1 ? 2 : 1;
     static_assert(NT * kDown == 2, "pairs");
     const int fr = lane & 15, second = (lane >> 4) & 1, col = (lane >> 5) * 8;
-#pragma unroll
-    for (int i = 0; i < MT; i += kDown)
-#pragma unroll
-        for (int h = 0; h < (kGate ? 1 : 2); ++h) {
-            float c[8], d[8];
-            pair_up(acc[i][h][0], acc[i + kDown - 1][h][NT - 1], c);
-            if (kGate) pair_up(acc[i][1][0], acc[i + kDown - 1][1][NT - 1], d);
-            finish<T, EPI>(w, p, tile.slice, m0 + wm * (BM / 2) + 16 * (i + (kDown - 1) * second) + fr,
-                           n0 + h * (BN / 2) + wn * (BN / 4) + 16 * (NT - 1) * second + col, c, d);
-        }
+    // unit u: half h = u % kHalves, rows i = u / kHalves * kDown
+    constexpr int kHalves = kGate ? 1 : 2, kUnits = MT / kDown * kHalves;
+    auto place = [&](int u) -> Place {
+        return {m0 + wm * (BM / 2) + 16 * (u / kHalves * kDown + (kDown - 1) * second) + fr,
+                n0 + u % kHalves * (BN / 2) + wn * (BN / 4) + 16 * (NT - 1) * second + col};
+    };
+    finish<T, EPI, kUnits>(w, p, tile.slice, place, [&](int u, float *c, float *d) {
+        const int i = u / kHalves * kDown, h = u % kHalves;
+        pair_up(acc[i][h][0], acc[i + kDown - 1][h][NT - 1], c);
+        if (kGate) pair_up(acc[i][1][0], acc[i + kDown - 1][1][NT - 1], d);
+    });
 }
 
 // bf16, tiles of 256 x 256, eight waves of 128 x 64: rows 64 wm .. of both halves of
@@ -371,9 +409,20 @@ __global__ __launch_bounds__(512) void k_product_large(Work w) {
 #pragma unroll
             for (int s = 0; s < 2; ++s) b[j][s] = lb.frag(j, s, at);
     };
+    // All but the last five panels have landed; stores: after those of the stores
+    // that a tile's end issued, at least kStores where they went ahead of none of
+    // the panels waited for.  (Memory instructions are counted in their order: a wait
+    // for ten would be one for the stores, which take as long as a step.)
+    constexpr int kStores = kGate ? 8 : kPlain == EPI ? 16 : 32;
+    auto landed = [&](bool stores) {
+        if (!stores) asm volatile("s_waitcnt vmcnt(10)" ::: "memory");
+        else if (kGate && w.gate) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(10 + 3 * 8) : "memory");
+        else asm volatile("s_waitcnt vmcnt(%0)" ::"n"(10 + kStores) : "memory");
+    };
     // the phase's reads have returned, and the next phase's panel has landed
-    auto meet_read = [&]() {
-        asm volatile("s_waitcnt vmcnt(10) lgkmcnt(0)" ::: "memory");
+    auto meet_read = [&](bool stores = false) {
+        landed(stores);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
@@ -398,6 +447,7 @@ __global__ __launch_bounds__(512) void k_product_large(Work w) {
         // All waves are done with the buffers: the next tile's first loads go ahead
         // of the stores of the one before.
         const Product before = p;
+        const bool whole = m0 + BM <= p.m && n0 + (kGate ? BN / 2 : BN) <= p.n;
         const int slice = tile.slice, row = m0 + wm * 64 + (lane & 15);
         const int col = n0 + wn * 32 + 16 * ((lane >> 4) & 1) + (lane >> 5) * 8;
         tile = spot(w, id);
@@ -425,21 +475,21 @@ __global__ __launch_bounds__(512) void k_product_large(Work w) {
             }
         }
         if (id != blockIdx.x) {
-#pragma unroll
-            for (int g = 0; g < 2; ++g)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int h = 0; h < (kGate ? 1 : 2); ++h) {
-                        float c[8], d[8];
-                        pair_up(acc[g][i][h][0], acc[g][i][h][1], c);
-                        if (kGate) pair_up(acc[g][i][1][0], acc[g][i][1][1], d);
-                        finish<T, EPI>(w, before, slice, row + g * 128 + 16 * i, col + h * 128, c, d);
-                    }
+            constexpr int kHalves = kGate ? 1 : 2;
+            finish<T, EPI, 8 * kHalves>(
+                w, before, slice,
+                [&](int u) -> Place {
+                    return {row + u / kHalves / 4 * 128 + 16 * (u / kHalves % 4), col + u % kHalves * 128};
+                },
+                [&](int u, float *c, float *d) {
+                    const f32x4_t(&r)[2][2] = acc[u / kHalves / 4][u / kHalves % 4];
+                    pair_up(r[u % kHalves][0], r[u % kHalves][1], c);
+                    if (kGate) pair_up(r[1][0], r[1][1], d);
+                });
         }
         if (tile.which < 0) break;
-        // the first two panels (and all but the last stores of the tile before)
-        asm volatile("s_waitcnt vmcnt(10)" ::: "memory");
+        const bool stores = id != blockIdx.x && whole;
+        landed(stores);
         __builtin_amdgcn_s_barrier();
         if (wave >= 4) __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
@@ -452,21 +502,21 @@ __global__ __launch_bounds__(512) void k_product_large(Work w) {
             read_a(at + kA0);
             read_b(b0, at + kB0);
             load_a(1, base + (kStage - at));
-            meet_read();
+            meet_read(stores && step == 0);
             multiply(acc[0], 0, b0);
             meet();
             read_b(b1, at + kB1);
             load_b(0, to);
-            meet_read();
+            meet_read(stores && step == 0);
             multiply(acc[0], 1, b1);
             meet();
             read_a(at + kA1);
             load_a(0, to);
-            meet_read();
+            meet_read(stores && step == 0);
             multiply(acc[1], 1, b1);
             meet();
             load_b(1, to);
-            meet_read();
+            meet_read(stores && step == 0);
             multiply(acc[1], 0, b0);
             meet();
             at = kStage - at;
