@@ -548,49 +548,75 @@ __global__ __launch_bounds__(256) void k_join_slices(Work w) {
 // ------------------------------------------------------------------------ plan
 
 // Tiles and slices of a launch of products with one contracted length.
-enum Tiles { kTiles256, kTiles128, kTiles64 };
+enum Tiles { kTiles256, kTiles128, kTiles64, kTiles64Deep };  // deep: four buffers for two
 struct Plan {
     Tiles kind;
     int slices, per_slice, steps;
     size_t partial;  // bytes
 };
-constexpr int kRowsOf[] = {256, 128, 64}, kColsOf[] = {256, 128, 64};
+constexpr int kSizeOf[] = {256, 128, 64, 64};
 struct Size {
     int64_t m, n;
 };
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 // Columns of a result that a tile holds.
-int cols_of(Tiles kind, Epilogue epi) { return epi == kGated ? kColsOf[kind] / 2 : kColsOf[kind]; }
+int cols_of(Tiles kind, Epilogue epi) { return epi == kGated ? kSizeOf[kind] / 2 : kSizeOf[kind]; }
 int64_t tiles_of(const Size &s, Tiles kind, Epilogue epi) {
-    return ceil_div(s.m, kRowsOf[kind]) * ceil_div(s.n, cols_of(kind, epi));
+    return ceil_div(s.m, kSizeOf[kind]) * ceil_div(s.n, cols_of(kind, epi));
 }
 
+// Microseconds of a launch, by which tiles and slices are chosen.  A CU moves about
+// 58 KB a microsecond into LDS, whatever the tile (bf16; 128: 32 KB a step, 0.5 us, or
+// 0.62 us for a block that has the CU to itself; 256: 64 KB in 1.4 us, all CUs being
+// busy), so that large tiles win where they fill the device and little of their time
+// goes into first loads and stores, which nothing covers there.  float32 is bound by
+// its products.  Measured against it (plain results, kernel times): 16,384 x 384, K
+// 1,536: 128 32 us (modelled 32), 256 42 (46), 64 39; 32,768 x 384: 256 46 (46), 128
+// 48 (50); three products of 1,536 x 384, K 16,384: 256 in 7 slices 68 + 10 (78), 128
+// in 4 72 + 7 (81), 64 in 4 113 + 7; 500 x 1,024, K 2,816: 64 in 4 slices 13 + 4 (19),
+// whole 23 (26), 128 whole 33 (35).
+struct Cost {
+    int resident;                              // blocks of a CU
+    double alone, shared;                      // a step of one block, and of each of several
+    double plain, gated, gated_saved, grad;  // first loads and results of a block, or of a CU's together
+};
+constexpr Cost kCost[2][4] = {
+    // float32
+    {{1, 0, 0, 0, 0, 0, 0}, {2, 2.0, 2.0, 3, 3, 6, 14}, {5, 0.63, 0.51, 3, 3, 4, 14}, {2, 0.6, 0.51, 2, 2, 3, 8}},
+    {{1, 1.4, 1.4, 7, 7, 12, 32}, {2, 0.62, 0.5, 3, 3, 6, 13}, {5, 0.4, 0.24, 3, 3, 4, 6}, {2, 0.26, 0.24, 2, 2, 3, 4}},
+};
+constexpr double kLaunch = 5.0, kJoin = 5.5, kJoinByte = 0.22e-6;
+
 // large: whether the largest tiles may be taken.
-Plan plan(const Size *sizes, int count, bool bf16, int64_t k, int segments, Epilogue epi, bool large = true) {
-    const int cus = compute_units(), elem = bf16 ? 2 : 4;
-    Plan p{};
-    auto tiles = [&](Tiles kind) {
-        int64_t n = 0;
-        for (int i = 0; i < count; ++i) n += tiles_of(sizes[i], kind, epi);
-        return n;
-    };
-    p.kind = bf16 && large && tiles(kTiles256) >= cus ? kTiles256 : tiles(kTiles128) >= cus ? kTiles128 : kTiles64;
-    p.slices = 1;
-    p.steps = int(ceil_div(k, 128 / elem)) * segments;
-    if (epi == kPlain) {
-        const int64_t n = tiles(p.kind);
-        // slices of four steps at least, until two blocks a CU
-        if (n < cus) p.slices = int(std::max<int64_t>(1, std::min<int64_t>(p.steps / 4, 2 * cus / std::max<int64_t>(n, 1))));
+Plan plan(const Size *sizes, int count, bool bf16, int64_t k, int segments, Epilogue epi, bool large, bool saved) {
+    const int64_t cus = compute_units(), steps = ceil_div(k, bf16 ? 64 : 32) * segments;
+    int64_t values = 0;
+    for (int i = 0; i < count; ++i) values += sizes[i].m * sizes[i].n;
+    Plan best{};
+    double least = 0;
+    for (Tiles kind : {kTiles256, kTiles128, kTiles64, kTiles64Deep}) {
+        if (kind == kTiles256 && !(bf16 && large)) continue;
+        const Cost &c = kCost[bf16][kind];
+        int64_t tiles = 0;
+        for (int i = 0; i < count; ++i) tiles += tiles_of(sizes[i], kind, epi);
+        const double ends = epi == kGated ? (saved ? c.gated_saved : c.gated) : epi == kGatedGrad ? c.grad : c.plain;
+        // slices of four steps at least
+        const int64_t most = epi == kPlain ? std::max<int64_t>(1, std::min<int64_t>(steps / 4, 32)) : 1;
+        for (int64_t slices = 1; slices <= most; ++slices) {
+            const int64_t each = ceil_div(steps, slices), blocks = ceil_div(tiles * slices, cus);
+            auto round = [&](int64_t n) { return n ? double(each) * std::max(c.alone, n * c.shared) + ends : 0.0; };
+            double t = kLaunch + double(blocks / c.resident) * round(c.resident) + round(blocks % c.resident);
+            if (slices > 1) t += kJoin + double(values) * slices * 4 * kJoinByte;
+            if (least == 0 || t < least) {
+                least = t;
+                best = Plan{kind, int(slices), int(each), int(steps), 0};
+            }
+        }
     }
-    p.per_slice = int(ceil_div(p.steps, p.slices));
-    p.slices = p.per_slice ? int(ceil_div(p.steps, p.per_slice)) : 1;
-    if (p.slices > 1) {
-        int64_t values = 0;
-        for (int i = 0; i < count; ++i) values += sizes[i].m * sizes[i].n;
-        p.partial = size_t(values) * p.slices * sizeof(float);
-    }
-    return p;
+    best.slices = best.per_slice ? int(ceil_div(best.steps, best.per_slice)) : 1;
+    if (best.slices > 1) best.partial = size_t(values) * best.slices * sizeof(float);
+    return best;
 }
 
 template <typename T, bool AK, bool BK, int EPI>
@@ -615,6 +641,7 @@ hipError_t launch(Work &w, const Plan &plan, float *partial, hipStream_t s) {
             if constexpr (sizeof(T) == 2) k_product_large<AK, BK, EPI><<<int(std::min<int64_t>(blocks, compute_units())), 512, 0, s>>>(w);
             break;
         case kTiles128: k_product<T, AK, BK, EPI, 128, 128, 2><<<grid, 256, 0, s>>>(w); break;
+        case kTiles64Deep: k_product<T, AK, BK, EPI, 64, 64, 4><<<grid, 256, 0, s>>>(w); break;
         case kTiles64: k_product<T, AK, BK, EPI, 64, 64, 2><<<grid, 256, 0, s>>>(w); break;
     }
     hipError_t e = hipGetLastError();
@@ -627,19 +654,19 @@ size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
 Plan plan_gated(const FfnArgs &a) {
     const Size s{a.rows, a.hidden};
-    return plan(&s, 1, a.bf16, a.channels, 1, kGated);
+    return plan(&s, 1, a.bf16, a.channels, 1, kGated, true, a.gate);
 }
 Plan plan_down(const FfnArgs &a) {
     const Size s{a.rows, a.channels};
-    return plan(&s, 1, a.bf16, a.hidden, 1, kPlain);
+    return plan(&s, 1, a.bf16, a.hidden, 1, kPlain, true, false);
 }
 Plan plan_dhidden(const FfnArgs &a) {
     const Size s{a.rows, a.hidden};
-    return plan(&s, 1, a.bf16, a.channels, 1, kGatedGrad);
+    return plan(&s, 1, a.bf16, a.channels, 1, kGatedGrad, true, false);
 }
 Plan plan_dx(const FfnArgs &a) {
     const Size s{a.rows, a.channels};
-    return plan(&s, 1, a.bf16, a.hidden, 2, kPlain, a.w_gate_s == a.w_up_s);
+    return plan(&s, 1, a.bf16, a.hidden, 2, kPlain, a.w_gate_s == a.w_up_s, false);
 }
 Plan plan_weights(const FfnArgs &a) {
     Size s[kMaxProducts];
@@ -647,7 +674,7 @@ Plan plan_weights(const FfnArgs &a) {
     if (a.dw_gate) s[n++] = {a.hidden, a.channels};
     if (a.dw_up) s[n++] = {a.hidden, a.channels};
     if (a.dw_down) s[n++] = {a.channels, a.hidden};
-    return plan(s, n, a.bf16, a.rows, 1, kPlain);
+    return plan(s, n, a.bf16, a.rows, 1, kPlain, true, false);
 }
 
 bool wants_hidden(const FfnArgs &a) { return a.dx || a.dw_gate || a.dw_up; }

@@ -852,14 +852,14 @@ def attention_grad_desc(fwd, dout, dq, dk, dv):
 
 
 def _matrix(d, name, x, shape, dtype, stride=None):
-    """Fill the pointer and row stride of tensor `name` of description d, [rows,
-    width] with contiguous rows; None entries of shape are free."""
+    """Fill the pointer and row stride of tensor `name` of description d, a matrix
+    of that shape with contiguous rows."""
     s = x.stride()
     if len(s) != 2 or (s[1] != 1 and x.shape[1] > 1):
         raise ValueError("%s must be [rows, width] with contiguous rows" % name)
     if x.dtype != dtype:
         raise ValueError("%s must have dtype %s" % (name, dtype))
-    if shape[0] not in (None, x.shape[0]) or shape[1] not in (None, x.shape[1]):
+    if x.shape != shape:
         raise ValueError("%s must have shape %s" % (name, tuple(shape)))
     _place(d, name, x)
     setattr(d, stride or name + "_stride", s[0])
