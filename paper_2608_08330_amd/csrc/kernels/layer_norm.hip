@@ -68,14 +68,37 @@ __device__ inline void load8_weight(const float *p, float *v) {
     for (int e = 0; e < 4; ++e) v[e] = a[e], v[e + 4] = b[e];
 }
 
+// x of another lane, by a pattern within its row of 16.
+template <int PATTERN>
+__device__ inline float from_lane(float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), PATTERN, 0xf, 0xf, true));
+}
+// Sum over the G <= 64 lanes of a group, in all of them: within rows of 16 by the
+// neighbour, the neighbouring pair and the mirrored half and row (whose lanes hold
+// equal sums), then rows by exchanges.  Through LDS a step would take 100 cycles.
+template <int G>
+__device__ inline float lane_sum(float x) {
+    if constexpr (G >= 2) x += from_lane<0xb1>(x);
+    if constexpr (G >= 4) x += from_lane<0x4e>(x);
+    if constexpr (G >= 8) x += from_lane<0x141>(x);
+    if constexpr (G >= 16) x += from_lane<0x140>(x);
+    if constexpr (G >= 32) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if constexpr (G >= 64) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+        x = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    return x;
+}
+
 // Sums of N values over the G threads of a row; `part` is LDS of a block's waves
 // (G > 64), used again only after the caller's next barrier.
 template <int G, int N>
 __device__ inline void row_sums(float (&x)[N], float (*part)[2]) {
 #pragma unroll
-    for (int n = 0; n < N; ++n)
-#pragma unroll
-        for (int d = 1; d < (G < 64 ? G : 64); d <<= 1) x[n] += __shfl_xor(x[n], d);
+    for (int n = 0; n < N; ++n) x[n] = lane_sum<(G < 64 ? G : 64)>(x[n]);
     if constexpr (G > 64) {
         const int wave = threadIdx.x / 64;
         if (threadIdx.x % 64 == 0)
@@ -152,35 +175,56 @@ __global__ __launch_bounds__(kThreads<G>) void k_layer_norm(LayerNormArgs a) {
 }
 
 // A block walks rows and keeps the sums of its channels' dw and db in registers;
-// partial: [blocks][2][channels].
-template <typename T, int G, int V>
-__global__ __launch_bounds__(kThreads<G>) void k_layer_norm_grad(LayerNormArgs a) {
+// the next row's loads are under way while a row's sums are made.  partial:
+// [blocks][2][channels].  PAST: with dsum.
+template <typename T, int G, int V, bool PAST>
+__global__ __launch_bounds__(kThreads<G>, 2) void k_layer_norm_grad(LayerNormArgs a) {
     constexpr int kRows = kThreads<G> / G;
+    constexpr int kTensors = PAST ? 3 : 2;
+    // two rows of float32 in four eights a channel would not fit the registers
+    constexpr bool kAhead = sizeof(T) == 2 || V * kTensors <= 8;
     __shared__ float part[3][G > 64 ? G / 64 : 1][2];
     const int l = threadIdx.x % G;
     const float over = 1.f / float(a.channels);
-    float dw[V][8] = {}, db[V][8] = {};
-    for (int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / G; row < a.rows; row += int64_t(gridDim.x) * kRows) {
-        Eight<T> x[V], dy[V], ds[V];
+    float dw[V][8] = {}, db[V][8] = {}, w[V][8];
+    Eight<T> x[V] = {}, dy[V] = {}, ds[V] = {};
+    auto fetch = [&](int64_t row) {
         const T *px = static_cast<const T *>(a.x) + row * a.x_s, *pg = static_cast<const T *>(a.dout) + row * a.dout_s;
-        const T *pd = static_cast<const T *>(a.residual) + row * a.residual_s;
+        const T *pd = PAST ? static_cast<const T *>(a.residual) + row * a.residual_s : nullptr;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int c = 8 * (l + G * v);
             if (c < a.channels) {
                 x[v].load(px + c);
                 dy[v].load(pg + c);
-                if (a.residual) ds[v].load(pd + c);
+                if (PAST) ds[v].load(pd + c);
             }
         }
-        float n[V][8], sum[1] = {}, square[1] = {}, dots[2] = {};
+    };
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int c = 8 * (l + G * v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[v][e] = 1.f;
+        if (a.weight && c < a.channels) load8_weight(a.weight + c, w[v]);
+    }
+    int64_t row = int64_t(blockIdx.x) * kRows + threadIdx.x / G;
+    const int64_t ahead = int64_t(gridDim.x) * kRows;
+    if (kAhead && row < a.rows) fetch(row);
+    for (; row < a.rows; row += ahead) {
+        if (!kAhead) fetch(row);
+        // channels past the end hold zeros
+        float n[V][8], y[V][8], past[V][8], sum[1] = {}, square[1] = {}, dots[2] = {};
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                n[v][e] = 8 * (l + G * v) < a.channels ? x[v][e] : 0.f;
+                n[v][e] = x[v][e];
+                y[v][e] = dy[v][e];
+                if (PAST) past[v][e] = ds[v][e];
                 sum[0] += n[v][e];
             }
+        if (kAhead && row + ahead < a.rows) fetch(row + ahead);
         row_sums<G>(sum, part[0]);
         const float mean = sum[0] * over;
 #pragma unroll
@@ -193,36 +237,27 @@ __global__ __launch_bounds__(kThreads<G>) void k_layer_norm_grad(LayerNormArgs a
         row_sums<G>(square, part[1]);
         const float scale = rsqrtf(fmaf(square[0], over, a.eps));
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int c = 8 * (l + G * v);
-            if (c >= a.channels) continue;
-            float w[8];
-            if (a.weight) load8_weight(a.weight + c, w);
+        for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 n[v][e] *= scale;
-                const float g = a.weight ? dy[v][e] * w[e] : dy[v][e];
-                dw[v][e] = fmaf(dy[v][e], n[v][e], dw[v][e]);
-                db[v][e] += dy[v][e];
-                dots[0] += g;
-                dots[1] = fmaf(g, n[v][e], dots[1]);
+                dw[v][e] = fmaf(y[v][e], n[v][e], dw[v][e]);
+                db[v][e] += y[v][e];
+                y[v][e] *= w[v][e];
+                dots[0] += y[v][e];
+                dots[1] = fmaf(y[v][e], n[v][e], dots[1]);
             }
-        }
         row_sums<G>(dots, part[2]);
         const float m0 = dots[0] * over, m1 = dots[1] * over;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int c = 8 * (l + G * v);
-            if (c >= a.channels) continue;
-            float w[8], y[8];
-            if (a.weight) load8_weight(a.weight + c, w);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float g = a.weight ? dy[v][e] * w[e] : dy[v][e];
-                y[e] = scale * (g - fmaf(n[v][e], m1, m0));
-                if (a.residual) y[e] += ds[v][e];
+                y[v][e] = scale * (y[v][e] - fmaf(n[v][e], m1, m0));
+                if (PAST) y[v][e] += past[v][e];
             }
-            store8(static_cast<T *>(a.out) + row * a.out_s + c, y);
+            if (c < a.channels) store8(static_cast<T *>(a.out) + row * a.out_s + c, y[v]);
         }
         if constexpr (G > 64) __syncthreads();  // the sums' LDS before the next row
     }
@@ -299,13 +334,14 @@ Cut cut(int channels) {
 
 int grad_blocks(const LayerNormArgs &a) {
     const int per = std::max(1, 256 / cut(a.channels).g);
-    return int(std::min<int64_t>(row_tiles(a.rows, per), 4 * compute_units()));
+    return int(std::min<int64_t>(row_tiles(a.rows, per), 2 * compute_units()));
 }
 
 template <typename T, int G, int V>
 hipError_t run(const LayerNormArgs &a, int grad_blocks, hipStream_t s) {
     if (grad_blocks) {
-        k_layer_norm_grad<T, G, V><<<grad_blocks, kThreads<G>, 0, s>>>(a);
+        if (a.residual) k_layer_norm_grad<T, G, V, true><<<grad_blocks, kThreads<G>, 0, s>>>(a);
+        else k_layer_norm_grad<T, G, V, false><<<grad_blocks, kThreads<G>, 0, s>>>(a);
     } else {
         const Fold f = fold(row_tiles(a.rows, kThreads<G> / G), kThreads<G>);
         k_layer_norm<T, G, V><<<dim3(f.x, 1, f.z), kThreads<G>, 0, s>>>(a);
