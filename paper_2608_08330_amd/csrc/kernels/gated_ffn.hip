@@ -526,6 +526,73 @@ __global__ __launch_bounds__(512) void k_product_large(Work w) {
     }
 }
 
+// Up to 16 rows: the weights are what is read, once, straight into registers.  A
+// block has COLS (8 or 16) columns of the result; its eight waves share the
+// contracted axis in turns of 128 bytes, kTurns of them under way at a time, and
+// their sums are added up through LDS in the waves' order.
+constexpr int kFewRows = 16;
+template <typename T, int EPI, int COLS>
+__global__ __launch_bounds__(512) void k_few(Work w) {
+    constexpr int kMats = EPI == kGated ? 2 : 1, kTurns = 4, kWaves = 8, kPer = 16 / int(sizeof(T)), kTurn = 128 / int(sizeof(T));
+    __shared__ f32x4_t sums[kWaves][kMats][64];
+    const Product &p = w.p[0];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, fk = lane >> 4;
+    const int n0 = int(blockIdx.x) * COLS;
+    // rows and columns past the end are read from the last one and not stored
+    const T *x = reinterpret_cast<const T *>(p.a[0] + int64_t(min(fr, p.m - 1)) * p.a_row) + fk * kPer;
+    const T *m[kMats];
+#pragma unroll
+    for (int i = 0; i < kMats; ++i)
+        m[i] = reinterpret_cast<const T *>(p.b[i] + int64_t(min(n0 + fr % COLS, p.n - 1)) * p.b_row[i]) + fk * kPer;
+    f32x4_t acc[kMats] = {};
+    for (int k0 = wave * kTurn; k0 < p.k; k0 += kWaves * kTurns * kTurn) {
+        u32x4_t a[kTurns][2] = {}, b[kTurns][2][kMats] = {};
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const int k = k0 + t * kWaves * kTurn + s * (kTurn / 2);
+                if (k + fk * kPer < p.k) {
+                    a[t][s] = *reinterpret_cast<const u32x4_t *>(x + k);
+#pragma unroll
+                    for (int i = 0; i < kMats; ++i) b[t][s][i] = *reinterpret_cast<const u32x4_t *>(m[i] + k);
+                }
+            }
+#pragma unroll
+        for (int t = 0; t < kTurns; ++t)
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int e = 0; e < kMmaSteps<T>; ++e)
+#pragma unroll
+                    for (int i = 0; i < kMats; ++i) acc[i] = mma(T(), e, b[t][s][i], a[t][s], acc[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kMats; ++i) sums[wave][i][lane] = acc[i];
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int i = 0; i < kMats; ++i)
+#pragma unroll
+        for (int v = 1; v < kWaves; ++v) acc[i] += sums[v][i][lane];
+    // four neighbouring columns of row fr
+    const int n = n0 + 4 * fk;
+    if (fr >= p.m || 4 * fk >= COLS || n >= p.n) return;
+    if constexpr (EPI == kGated) {
+        f32x4_t h;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = activation(w.gelu, acc[0][e], nullptr) * acc[1][e];
+        const int64_t to = fr * w.hidden_s + n;
+        store4(static_cast<T *>(w.act) + to, h);
+        if (w.gate) {
+            store4(static_cast<T *>(w.gate) + to, acc[0]);
+            store4(static_cast<T *>(w.up) + to, acc[1]);
+        }
+    } else {
+        store4(static_cast<T *>(p.c) + fr * p.c_row + n, acc[0]);
+    }
+}
+
 // Adds up the slices in their order and rounds.
 template <typename T>
 __global__ __launch_bounds__(256) void k_join_slices(Work w) {
@@ -650,6 +717,15 @@ hipError_t launch(Work &w, const Plan &plan, float *partial, hipStream_t s) {
     return hipGetLastError();
 }
 
+// Eight columns a block where sixteen would leave CUs without one.
+template <typename T, int EPI>
+hipError_t launch_few(const Work &w, hipStream_t s) {
+    const int n = w.p[0].n;
+    if (ceil_div(n, 16) < compute_units()) k_few<T, EPI, 8><<<int(ceil_div(n, 8)), 512, 0, s>>>(w);
+    else k_few<T, EPI, 16><<<int(ceil_div(n, 16)), 512, 0, s>>>(w);
+    return hipGetLastError();
+}
+
 size_t round16(size_t n) { return (n + 15) / 16 * 16; }
 
 Plan plan_gated(const FfnArgs &a) {
@@ -699,7 +775,8 @@ hipError_t forward(FfnArgs a, hipStream_t s) {
     p.a_row = uint32_t(a.x_s * sizeof(T));
     p.b_row[0] = uint32_t(a.w_gate_s * sizeof(T)), p.b_row[1] = uint32_t(a.w_up_s * sizeof(T));
     p.m = a.rows, p.n = a.hidden, p.k = a.channels;
-    hipError_t e = launch<T, true, true, kGated>(w, plan_gated(a), nullptr, s);
+    const bool few = a.rows <= kFewRows;
+    hipError_t e = few ? launch_few<T, kGated>(w, s) : launch<T, true, true, kGated>(w, plan_gated(a), nullptr, s);
     if (e != hipSuccess) return e;
     p = Product{};
     p.a[0] = static_cast<const char *>(a.act);
@@ -707,7 +784,8 @@ hipError_t forward(FfnArgs a, hipStream_t s) {
     p.a_row = uint32_t(a.hidden_s * sizeof(T)), p.b_row[0] = uint32_t(a.w_down_s * sizeof(T));
     p.m = a.rows, p.n = a.channels, p.k = a.hidden;
     p.c = a.out, p.c_row = a.out_s;
-    return launch<T, true, true, kPlain>(w, plan_down(a), reinterpret_cast<float *>(space), s);
+    return few ? launch_few<T, kPlain>(w, s)
+               : launch<T, true, true, kPlain>(w, plan_down(a), reinterpret_cast<float *>(space), s);
 }
 
 template <typename T>
@@ -762,7 +840,7 @@ hipError_t gradient(const FfnArgs &a, hipStream_t s) {
 
 size_t gated_ffn_workspace(const FfnArgs &a) {
     if (a.rows == 0) return 0;
-    return (a.act ? 0 : round16(hidden_bytes(a))) + plan_down(a).partial;
+    return (a.act ? 0 : round16(hidden_bytes(a))) + (a.rows <= kFewRows ? 0 : plan_down(a).partial);
 }
 
 int gated_ffn(const FfnArgs &a, void *stream) {

@@ -68,6 +68,15 @@ __device__ inline void load8(const float *p, float *v) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = a[e], v[e + 4] = b[e];
 }
+// Four of them.
+__device__ inline void store4(uint16_t *p, f32x4_t v) {
+    typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+    bf16x4_t b;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) b[e] = __bf16(v[e]);
+    *reinterpret_cast<bf16x4_t *>(p) = b;
+}
+__device__ inline void store4(float *p, f32x4_t v) { *reinterpret_cast<f32x4_t *>(p) = v; }
 // Two results side by side, x and y, as eight neighbouring columns a lane: of x
 // where fk is even and of y where it is odd, from column 8 (fk / 2) on.
 __device__ inline void pair_up(f32x4_t x, f32x4_t y, float *v) {

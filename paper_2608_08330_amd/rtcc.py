@@ -854,15 +854,15 @@ def attention_grad_desc(fwd, dout, dq, dk, dv):
 def _matrix(d, name, x, shape, dtype, stride=None):
     """Fill the pointer and row stride of tensor `name` of description d, a matrix
     of that shape with contiguous rows."""
-    s = x.stride()
-    if len(s) != 2 or (s[1] != 1 and x.shape[1] > 1):
-        raise ValueError("%s must be [rows, width] with contiguous rows" % name)
     if x.dtype != dtype:
         raise ValueError("%s must have dtype %s" % (name, dtype))
     if x.shape != shape:
         raise ValueError("%s must have shape %s" % (name, tuple(shape)))
+    row, step = x.stride()
+    if step != 1 and shape[1] > 1:
+        raise ValueError("%s must have contiguous rows" % name)
     _place(d, name, x)
-    setattr(d, stride or name + "_stride", s[0])
+    setattr(d, stride or name + "_stride", row)
 
 
 def layer_norm_desc(x, out, weight=None, bias=None, residual=None, sum_out=None, eps=1e-5):
