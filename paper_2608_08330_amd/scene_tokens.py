@@ -1,11 +1,14 @@
-"""One attention layer over tokens of the bird's-eye-view map, frame after frame.
+"""One attention layer, or a whole block, over tokens of the bird's-eye-view map,
+frame after frame.
 
-  python -m paper_2608_08330_amd.scene_tokens [--frames F] [--patches P]
+  python -m paper_2608_08330_amd.scene_tokens [--frames F] [--patches P] [--hidden H]
 
 Runs the token operators together as a program uses them: `train` normalises
 and rotates queries and keys by (time, row, column), attends causally over the
 scene's packed history and takes the gradients back to the projection;
-`serve` appends the newest frame's tokens to a cache and attends to it.  The
+`serve` appends the newest frame's tokens to a cache and attends to it.  With
+--hidden the layer stands in a block: layer norm, attention, layer norm of the
+sum, gated feed-forward unit, and the gradients of all of them.  The
 projections are torch products.  A served token sees what it saw in `train`,
 so both answers agree up to the stored type's rounding; main() prints how far
 they differ.
@@ -50,17 +53,22 @@ class SceneAttention:
         R.rtcc_attention(d, space.data_ptr(), space.numel(), torch.cuda.current_stream().cuda_stream)
         return out, lse, d
 
-    def train(self, tokens, positions, offsets, dout):
-        """tokens [n, channels] of packed scenes, positions float32 [n, 3],
-        offsets int32 [scenes + 1], dout [n, q_heads, dim]: outputs, and the
-        gradients of the projection and of both norm weights."""
+    def forward(self, tokens, positions, offsets):
+        """Outputs [n, q_heads, dim], and what `backward` needs."""
         stream = torch.cuda.current_stream().cuda_stream
         q, k, v = self._split(tokens @ self.weight)
         qr, kr = torch.empty(q.shape, dtype=q.dtype, device="cuda"), torch.empty(k.shape, dtype=k.dtype, device="cuda")
         rope = R.norm_rope_desc(q, k, qr, kr, self.q_norm, self.k_norm, positions, self.inv_freq, self.sections)
         R.rtcc_norm_rope(rope, stream)
-        out, _lse, d = self._attend(qr, kr, v, offsets, offsets, None)
-        flat = torch.empty(tokens.shape[0], self.weight.shape[1], dtype=q.dtype, device="cuda")
+        out, lse, d = self._attend(qr, kr, v, offsets, offsets, None)
+        return out, (tokens, rope, d, (q, k, v, qr, kr, out, lse, positions, offsets))
+
+    def backward(self, saved, dout):
+        """Gradients of the projection's outputs (dtokens = that @ weight.t()), of
+        the projection and of both norm weights."""
+        tokens, rope, d, kept = saved
+        stream = torch.cuda.current_stream().cuda_stream
+        flat = torch.empty(tokens.shape[0], self.weight.shape[1], dtype=kept[0].dtype, device="cuda")
         dq, dk, dv = self._split(flat)
         g = R.attention_grad_desc(d, dout, dq, dk, dv)
         space = _space(R.rtcc_attention_grad_workspace(g), "cuda")
@@ -69,7 +77,14 @@ class SceneAttention:
         g = R.norm_rope_grad_desc(rope, dq, dk, dq, dk, dwq, dwk)  # in place
         space = _space(R.rtcc_norm_rope_grad_workspace(g), "cuda")
         R.rtcc_norm_rope_grad(g, space.data_ptr(), space.numel(), stream)
-        return out, tokens.t().contiguous() @ flat, dwq, dwk
+        return flat, tokens.t().contiguous() @ flat, dwq, dwk
+
+    def train(self, tokens, positions, offsets, dout):
+        """tokens [n, channels] of packed scenes, positions float32 [n, 3],
+        offsets int32 [scenes + 1], dout [n, q_heads, dim]: outputs, and the
+        gradients of the projection and of both norm weights."""
+        out, saved = self.forward(tokens, positions, offsets)
+        return (out,) + self.backward(saved, dout)[1:]
 
     def serve(self, tokens, positions, cache_k, cache_v, length):
         """Append tokens [n, channels] after `length` rows of a scene's cache
@@ -88,20 +103,101 @@ class SceneAttention:
                             torch.tensor([length + n], **i32))[0]
 
 
+class SceneBlock:
+    """y = x + proj(attention(norm1(x))), and with the gated feed-forward unit the
+    stream y + unit(norm2(y)).  Parameters are a dict of tensors; `train` returns
+    gradients under the same names."""
+
+    def __init__(self, channels, q_heads, kv_heads, dim, hidden, softcap=30.0, dtype=torch.bfloat16, seed=0):
+        self.attention = SceneAttention(channels, q_heads, kv_heads, dim, softcap, dtype, seed)
+        gen = torch.Generator().manual_seed(seed + 1)
+
+        def matrix(rows, width, fan):
+            return (torch.randn(rows, width, generator=gen) * fan ** -0.5).to("cuda", dtype)
+
+        both = matrix(2 * hidden, channels, channels)  # of one product, as the operator reads them
+        self.p = dict(qkv=self.attention.weight, q_norm=self.attention.q_norm, k_norm=self.attention.k_norm,
+                      proj=matrix(q_heads * dim, channels, q_heads * dim),
+                      w_gate=both[:hidden], w_up=both[hidden:], w_down=matrix(channels, hidden, hidden),
+                      **{"%s%d" % (n, i): (torch.ones if n == "weight" else torch.zeros)(channels, device="cuda")
+                         for n in ("weight", "bias") for i in (1, 2)})
+
+    def _norm(self, x, i, residual=None):
+        """norm i of x (+ residual): the normed rows, the sum, the description."""
+        out = torch.empty_like(x)
+        total = x if residual is None else torch.empty_like(x)
+        d = R.layer_norm_desc(x, out, self.p["weight%d" % i], self.p["bias%d" % i], residual=residual,
+                              sum_out=None if residual is None else total)
+        R.rtcc_layer_norm(d, torch.cuda.current_stream().cuda_stream)
+        return out, total, d
+
+    def _norm_grad(self, d, i, dout, dsum, grads):
+        """Gradient of norm i's input, dsum of the sum past it added."""
+        dx = torch.empty_like(dout)
+        dw, db = torch.empty_like(self.p["weight%d" % i]), torch.empty_like(self.p["bias%d" % i])
+        g = R.layer_norm_grad_desc(d, dout, dx, dsum=dsum, dweight=dw, dbias=db)
+        space = _space(R.rtcc_layer_norm_grad_workspace(g), "cuda")
+        R.rtcc_layer_norm_grad(g, space.data_ptr(), space.numel(), torch.cuda.current_stream().cuda_stream)
+        grads["weight%d" % i], grads["bias%d" % i] = dw, db
+        return dx
+
+    def _unit(self, x, **saved):
+        out = torch.empty_like(x)
+        d = R.gated_ffn_desc(x, self.p["w_gate"], self.p["w_up"], self.p["w_down"], out, **saved)
+        space = _space(R.rtcc_gated_ffn_workspace(d), x.device)
+        R.rtcc_gated_ffn(d, space.data_ptr(), space.numel(), torch.cuda.current_stream().cuda_stream)
+        return out, d
+
+    def train(self, x, positions, offsets, dstream):
+        """x [n, channels] of packed scenes and dstream, the gradient of the new
+        stream: that stream, and the gradients (of x under "x")."""
+        n, hidden = x.shape[0], self.p["w_gate"].shape[0]
+        a, _, norm1 = self._norm(x, 1)
+        heads, saved = self.attention.forward(a, positions, offsets)
+        flat = heads.reshape(n, -1)
+        b, y, norm2 = self._norm(flat @ self.p["proj"], 2, x)
+        kept = {k: torch.empty(n, hidden, dtype=x.dtype, device="cuda") for k in ("gate", "up", "act")}
+        f, unit = self._unit(b, **kept)
+
+        grads = {k: torch.empty_like(self.p[k]) for k in ("w_gate", "w_up", "w_down")}
+        db = torch.empty_like(b)
+        g = R.gated_ffn_grad_desc(unit, dstream, db, grads["w_gate"], grads["w_up"], grads["w_down"])
+        space = _space(R.rtcc_gated_ffn_grad_workspace(g), "cuda")
+        R.rtcc_gated_ffn_grad(g, space.data_ptr(), space.numel(), torch.cuda.current_stream().cuda_stream)
+        dy = self._norm_grad(norm2, 2, db, dstream, grads)
+        grads["proj"] = flat.t().contiguous() @ dy
+        dheads = (dy @ self.p["proj"].t().contiguous()).view(heads.shape)
+        dqkv, grads["qkv"], grads["q_norm"], grads["k_norm"] = self.attention.backward(saved, dheads)
+        grads["x"] = self._norm_grad(norm1, 1, dqkv @ self.p["qkv"].t().contiguous(), dy, grads)
+        return y + f, grads
+
+    def serve(self, x, positions, cache_k, cache_v, length):
+        """The new stream of a frame's tokens x, after `length` rows of a cache."""
+        a, _, _ = self._norm(x, 1)
+        heads = self.attention.serve(a, positions, cache_k, cache_v, length)
+        b, y, _ = self._norm(heads.reshape(x.shape[0], -1) @ self.p["proj"], 2, x)
+        return y + self._unit(b)[0]
+
+
 def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     ap.add_argument("--frames", type=int, default=4)
     ap.add_argument("--patches", type=int, default=8, help="patches a side of the map")
     ap.add_argument("--channels", type=int, default=384)
+    ap.add_argument("--hidden", type=int, default=0, help="hidden channels of a whole block; 0: attention alone")
     a = ap.parse_args(argv)
     per, n = a.patches ** 2, a.frames * a.patches ** 2
     gen = torch.Generator().manual_seed(1)
-    layer = SceneAttention(a.channels, 6, 2, 64)
     tokens = torch.randn(n, a.channels, generator=gen).to("cuda", torch.bfloat16)
     i = torch.arange(n, device="cuda")
     positions = torch.stack([i // per, i % per // a.patches, i % a.patches], dim=1).float()
-    dout = torch.randn(n, 6, 64, generator=gen).to("cuda", torch.bfloat16)
-    out, dw, _dwq, _dwk = layer.train(tokens, positions, torch.tensor([0, n], dtype=torch.int32, device="cuda"), dout)
+    if a.hidden:
+        layer, width = SceneBlock(a.channels, 6, 2, 64, a.hidden), (a.channels,)
+    else:
+        layer, width = SceneAttention(a.channels, 6, 2, 64), (6, 64)
+    dout = torch.randn(n, *width, generator=gen).to("cuda", torch.bfloat16)
+    result = layer.train(tokens, positions, torch.tensor([0, n], dtype=torch.int32, device="cuda"), dout)
+    out, dw = result[0], result[1]["qkv"] if a.hidden else result[1]
     cache = [torch.zeros(n, 2, 64, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
     served = torch.cat([layer.serve(tokens[f:f + per], positions[f:f + per], cache[0], cache[1], f)
                         for f in range(0, n, per)])
