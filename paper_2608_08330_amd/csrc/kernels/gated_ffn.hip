@@ -195,7 +195,7 @@ __device__ inline void finish(const Work &w, const Product &p, int slice, At at,
 // one half's are read while the other's are multiplied.  Reads and loads stand
 // between the products, so that one wave on a SIMD keeps all units busy.
 template <typename T, bool AK, bool BK, int EPI, int BM, int BN, int STAGES>
-__global__ __launch_bounds__(256, 2) void k_product(Work w) {
+__global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_product(Work w) {
     constexpr int MT = BM / 32, NT = BN / 64;
     constexpr bool kGate = EPI == kGated, kTwo = EPI == kPlain && AK && !BK;  // kTwo: two segments
     typedef Panel<T, AK, BM> PA;
@@ -305,8 +305,13 @@ __global__ __launch_bounds__(256, 2) void k_product(Work w) {
             else prepare();
         });
         meet();
+        // bf16: loads first, each with a read: they have the longer way.  float32,
+        // whose products take 16 times as long, has the reads first.
         multiply(1, kReads + kLoads, [&](int n) {
-            if (n < kReads) read(n, 0, then);
+            constexpr int kBoth = sizeof(T) == 2 ? 2 * (kReads < kLoads ? kReads : kLoads) : 0;
+            if (n < kBoth && n % 2 == 0) load(n / 2, base + at);
+            else if (n < kBoth) read(n / 2, 0, then);
+            else if (n < kReads + kBoth / 2) read(n - kBoth / 2, 0, then);
             else load(n - kReads, base + at);
         });
         at = then;
@@ -314,19 +319,20 @@ __global__ __launch_bounds__(256, 2) void k_product(Work w) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load into LDS outlives the block
 
     // pairs of tiles side by side, or below each other where there is one
-    constexpr int kDown = NT == 1 ? 2 : 1;
-    static_assert(NT * kDown == 2, "pairs");
+    constexpr int kDown = NT == 1 ? 2 : 1, kAcross = NT == 1 ? 1 : NT / 2;
     const int fr = lane & 15, second = (lane >> 4) & 1, col = (lane >> 5) * 8;
-    // unit u: half h = u % kHalves, rows i = u / kHalves * kDown
-    constexpr int kHalves = kGate ? 1 : 2, kUnits = MT / kDown * kHalves;
+    // unit u: pair j = u % kAcross of half h, rows i
+    constexpr int kHalves = kGate ? 1 : 2, kUnits = MT / kDown * kHalves * kAcross;
     auto place = [&](int u) -> Place {
-        return {m0 + wm * (BM / 2) + 16 * (u / kHalves * kDown + (kDown - 1) * second) + fr,
-                n0 + u % kHalves * (BN / 2) + wn * (BN / 4) + 16 * (NT - 1) * second + col};
+        const int j = u % kAcross, h = u / kAcross % kHalves, i = u / kAcross / kHalves * kDown;
+        return {m0 + wm * (BM / 2) + 16 * (i + (kDown - 1) * second) + fr,
+                n0 + h * (BN / 2) + wn * (BN / 4) + 32 * j + 16 * (2 - kDown) * second + col};
     };
     finish<T, EPI, kUnits>(w, p, tile.slice, place, [&](int u, float *c, float *d) {
-        const int i = u / kHalves * kDown, h = u % kHalves;
-        pair_up(acc[i][h][0], acc[i + kDown - 1][h][NT - 1], c);
-        if (kGate) pair_up(acc[i][1][0], acc[i + kDown - 1][1][NT - 1], d);
+        const int j = u % kAcross, h = u / kAcross % kHalves, i = u / kAcross / kHalves * kDown;
+        constexpr int kNext = NT == 1 ? 0 : 1;
+        pair_up(acc[i][h][2 * j], acc[i + kDown - 1][h][2 * j + kNext], c);
+        if (kGate) pair_up(acc[i][1][2 * j], acc[i + kDown - 1][1][2 * j + kNext], d);
     });
 }
 
@@ -668,8 +674,8 @@ Plan plan(const Size *sizes, int count, bool bf16, int64_t k, int segments, Epil
         int64_t tiles = 0;
         for (int i = 0; i < count; ++i) tiles += tiles_of(sizes[i], kind, epi);
         const double ends = epi == kGated ? (saved ? c.gated_saved : c.gated) : epi == kGatedGrad ? c.grad : c.plain;
-        // slices of four steps at least
-        const int64_t most = epi == kPlain ? std::max<int64_t>(1, std::min<int64_t>(steps / 4, 32)) : 1;
+        // slices of four steps at least, where the tiles are few
+        const int64_t most = epi == kPlain && tiles <= 4 * cus ? std::max<int64_t>(1, std::min<int64_t>(steps / 4, 32)) : 1;
         for (int64_t slices = 1; slices <= most; ++slices) {
             const int64_t each = ceil_div(steps, slices), blocks = ceil_div(tiles * slices, cus);
             auto round = [&](int64_t n) { return n ? double(each) * std::max(c.alone, n * c.shared) + ends : 0.0; };

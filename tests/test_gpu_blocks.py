@@ -270,7 +270,7 @@ def test_layer_norm_gradients_of_no_rows():
 # ---------------------------------------------------------- gated feed-forward
 
 class Unit:
-    def __init__(self, precision, rows, channels, hidden, gelu, pad=0, seed=0, saved=True):
+    def __init__(self, precision, rows, channels, hidden, gelu, pad=0, seed=0, saved=True, apart=False):
         import torch
         gen = torch.Generator().manual_seed(seed)
         self.precision, self.gelu, self.pad, self.shape = precision, gelu, pad, (rows, channels, hidden)
@@ -280,9 +280,12 @@ class Unit:
         self.wd = _rand(gen, channels, hidden, precision, hidden ** -0.5)
         self.dy = _rand(gen, rows, channels, precision)
         self.gx, self.gdy, self.gwd = (self.guarded(t) for t in (self.x, self.dy, self.wd))
-        both = Guarded(2 * hidden, channels, _dtype(precision), pad, torch.cat([self.wg, self.wu]))
-        self.both = both
-        self.gwg, self.gwu = both.x[:hidden], both.x[hidden:]
+        if apart:  # rows of the two weights differently far apart
+            self.both = [Guarded(hidden, channels, _dtype(precision), p, w) for p, w in ((8, self.wg), (24, self.wu))]
+            self.gwg, self.gwu = (b.x for b in self.both)
+        else:
+            self.both = Guarded(2 * hidden, channels, _dtype(precision), pad, torch.cat([self.wg, self.wu]))
+            self.gwg, self.gwu = self.both.x[:hidden], self.both.x[hidden:]
         self.out = self.matrix(rows, channels)
         self.saved = [self.matrix(rows, hidden) for _ in range(3)] if saved else [None] * 3
 
@@ -379,9 +382,12 @@ UNIT = [
     (1, 8, 8), (1, 384, 1536), (2, 72, 40), (5, 1032, 264), (16, 64, 64), (17, 328, 1000), (33, 2056, 136), (63, 128, 2056),
     (64, 256, 512), (65, 264, 520), (128, 128, 128), (129, 136, 264), (200, 24, 1104), (300, 512, 72), (1000, 200, 328),
     (2100, 40, 2056), (4200, 1032, 24), (5000, 16, 16), (35, 1032, 2056),
-    # the largest tiles: of the hidden layer, of the rows, of the weights
     (4200, 328, 2056), (8400, 2056, 264), (600, 2056, 4104),
 ]
+
+# The largest tiles, in every product, several a block: with a part of the last
+# tile and step in each of the two segments of dx; and the weights' in slices.
+LARGE = [(8100, 2048, 2040), (16000, 384, 1536)]
 
 
 @pytest.mark.parametrize("precision", PRECISIONS)
@@ -400,6 +406,30 @@ def test_gated_ffn_gradient(precision, rows, channels, hidden):
         first = [t.x.clone() for t in c.grads]
         c.gradients()
         assert all(torch.equal(a, t.x) for a, t in zip(first, c.grads))
+
+
+@pytest.mark.parametrize("rows,channels,hidden", LARGE)
+def test_large_gated_ffn_and_gradient(rows, channels, hidden):
+    import torch
+    c = Unit("bf16", rows, channels, hidden, rows > 10000, 8).forward()
+    some = np.unique(np.concatenate([np.arange(300), np.arange(rows - 200, rows), np.arange(0, rows, 61)]))
+    c.check(some).gradients().check_gradients()
+    first = [t.x.clone() for t in c.grads + c.saved + [c.out]]
+    for _ in range(3):
+        c.forward().gradients()
+        assert all(torch.equal(a, t.x) for a, t in zip(first, c.grads + c.saved + [c.out]))
+
+
+@pytest.mark.parametrize("precision", PRECISIONS)
+@pytest.mark.parametrize("rows,channels,hidden", [(3, 72, 40), (40, 136, 72), (700, 264, 520)])
+def test_weights_of_two_strides(precision, rows, channels, hidden):
+    Unit(precision, rows, channels, hidden, False, apart=True).forward().check().gradients().check_gradients()
+
+
+def test_large_tiles_with_weights_of_two_strides():
+    """As many tiles as the largest ones fill, but for the stride of dx's weights."""
+    c = Unit("bf16", 8100, 2048, 520, False, apart=True).forward()
+    c.check(np.arange(0, 8100, 27)).gradients().check_gradients()
 
 
 @pytest.mark.parametrize("precision", PRECISIONS)
