@@ -57,7 +57,10 @@ __device__ inline float gelu(float z, float *slope) {
     if (slope) *slope = fmaf(z, 0.3989422804014327f * e, phi);
     return z * phi;
 }
-__device__ inline float activation(bool is_gelu, float z, float *slope) { return is_gelu ? gelu(z, slope) : silu(z, slope); }
+template <bool GELU>
+__device__ inline float activation(float z, float *slope) {
+    return GELU ? gelu(z, slope) : silu(z, slope);
+}
 
 // -------------------------------------------------------------------- products
 
@@ -67,7 +70,7 @@ struct Product {
     const char *a[2], *b[2];  // of each segment; of a gated product b are the halves of a tile's columns
     uint32_t a_row, b_row[2];  // bytes between rows
     int32_t m, n, k;           // k: of a segment
-    int32_t tiles_n, tiles;
+    int32_t tiles_m, tiles_n, tiles;
     void *c;
     int64_t c_row;  // elements
     int64_t partial;  // floats before the product's part of a slice
@@ -95,24 +98,31 @@ struct Spot {
 };
 constexpr int kBand = 4;
 __device__ inline Spot spot(const Work &w, uint32_t id) {
-    int which = 0;
-    uint32_t tiles = w.p[0].tiles, across = w.p[0].tiles_n;
+    int which = 0, slice = 0;
+    uint32_t tiles = w.p[0].tiles, across = w.p[0].tiles_n, down = w.p[0].tiles_m;
+    if (w.products > 1) {
 #pragma unroll
-    for (int i = 1; i < kMaxProducts; ++i)
-        if (which == i - 1 && i < w.products && id >= tiles * w.slices) {
-            id -= tiles * w.slices;
-            which = i, tiles = w.p[i].tiles, across = w.p[i].tiles_n;
-        }
+        for (int i = 1; i < kMaxProducts; ++i)
+            if (which == i - 1 && i < w.products && id >= tiles * w.slices) {
+                id -= tiles * w.slices;
+                which = i, tiles = w.p[i].tiles, across = w.p[i].tiles_n, down = w.p[i].tiles_m;
+            }
+    }
     const uint32_t n = tiles * w.slices, x = id % 8;
     if (id >= n) return {-1, 0, 0, 0};
     id = x * (n / 8) + min(x, n % 8) + id / 8;
-    const int slice = int(id / tiles);
-    id %= tiles;
-    const uint32_t down = tiles / across, top = id / (kBand * across) * kBand, rows = min(down - top, uint32_t(kBand));
+    if (w.slices > 1) {
+        slice = int(id / tiles);
+        id -= slice * tiles;
+    }
+    // one division where the band is whole: each costs some 40 instructions, and a
+    // tile of the smallest step counts takes a few thousand cycles
+    const uint32_t top = id / (kBand * across) * kBand, rows = min(down - top, uint32_t(kBand));
     id -= top * across;
+    const uint32_t n_at = rows == kBand ? id / kBand : id / rows;
     // said to be uniform, so that all addresses stay in scalar registers
     return {__builtin_amdgcn_readfirstlane(which), __builtin_amdgcn_readfirstlane(slice),
-            __builtin_amdgcn_readfirstlane(top + id % rows), __builtin_amdgcn_readfirstlane(id / rows)};
+            __builtin_amdgcn_readfirstlane(top + (id - n_at * rows)), __builtin_amdgcn_readfirstlane(n_at)};
 }
 // A copy by constant indexes: an indexed one would go through memory.
 __device__ inline Product pick(const Work &w, int which) { return which == 0 ? w.p[0] : which == 1 ? w.p[1] : w.p[2]; }
@@ -124,21 +134,21 @@ struct Place {
 
 // Stores a lane's UNITS results; at(u) is the place of the u-th, take(u, c, d) gives
 // its values c (a gated product's: of gate, with those of up in d).
-template <typename T, int EPI, int UNITS, class At, class Take>
-__device__ inline void finish(const Work &w, const Product &p, int slice, At at, Take take) {
+template <typename T, int EPI, int UNITS, bool GELU, class At, class Take>
+__device__ inline void finish_with(const Work &w, const Product &p, int slice, At at, Take take) {
     if constexpr (EPI == kGatedGrad) {
         // g and u a batch ahead: the loads are waited for together, from places
         // that always exist
-        constexpr int kBatch = UNITS < 4 ? UNITS : 4, kBatches = UNITS / kBatch;
+        constexpr int kBatch = UNITS == 8 ? 4 : 2, kBatches = UNITS / kBatch;  // as the registers allow
         static_assert(UNITS % kBatch == 0, "whole batches");
-        float g[2][kBatch][8], u[2][kBatch][8];
+        Eight<T> g[2][kBatch], u[2][kBatch];
         auto fetch = [&](int b) {
 #pragma unroll
             for (int i = 0; i < kBatch; ++i) {
                 const Place o = at(b * kBatch + i);
                 const int64_t from = min(o.m, p.m - 1) * w.hidden_s + min(o.n, p.n - 8);
-                load8(static_cast<const T *>(w.gate) + from, g[b & 1][i]);
-                load8(static_cast<const T *>(w.up) + from, u[b & 1][i]);
+                g[b & 1][i].load(static_cast<const T *>(w.gate) + from);
+                u[b & 1][i].load(static_cast<const T *>(w.up) + from);
             }
         };
         fetch(0);
@@ -154,13 +164,14 @@ __device__ inline void finish(const Work &w, const Product &p, int slice, At at,
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     float slope;
-                    du[e] = c[e] * activation(w.gelu, g[b & 1][i][e], &slope);
+                    du[e] = c[e] * activation<GELU>(g[b & 1][i][e], &slope);
                     dg[e] = c[e] * u[b & 1][i][e] * slope;
                 }
                 if (o.m >= p.m || o.n >= p.n) continue;
                 const int64_t to = int64_t(o.m) * p.n + o.n;
                 store8(static_cast<T *>(p.c) + to, dg);
                 store8(static_cast<T *>(p.c) + int64_t(p.m) * p.n + to, du);
+                __builtin_amdgcn_sched_barrier(0);  // more at once would not fit the registers
             }
         }
     } else {
@@ -172,7 +183,7 @@ __device__ inline void finish(const Work &w, const Product &p, int slice, At at,
             if constexpr (EPI == kGated) {
                 float h[8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) h[e] = activation(w.gelu, c[e], nullptr) * d[e];
+                for (int e = 0; e < 8; ++e) h[e] = activation<GELU>(c[e], nullptr) * d[e];
                 if (o.m >= p.m || o.n >= p.n) continue;
                 const int64_t to = o.m * w.hidden_s + o.n;
                 store8(static_cast<T *>(w.act) + to, h);
@@ -185,8 +196,16 @@ __device__ inline void finish(const Work &w, const Product &p, int slice, At at,
                 if (w.slices > 1) store8(w.partial + slice * w.slice_size + p.partial + int64_t(o.m) * p.n + o.n, c);
                 else store8(static_cast<T *>(p.c) + o.m * p.c_row + o.n, c);
             }
+            if (EPI == kGated) __builtin_amdgcn_sched_barrier(0);
         }
     }
+}
+
+// One branch for all of a lane's results: with one for each, no two of them overlap.
+template <typename T, int EPI, int UNITS, class At, class Take>
+__device__ inline void finish(const Work &w, const Product &p, int slice, At at, Take take) {
+    if (EPI != kPlain && w.gelu) finish_with<T, EPI, UNITS, true>(w, p, slice, at, take);
+    else finish_with<T, EPI, UNITS, false>(w, p, slice, at, take);
 }
 
 // Columns of a tile lie in two halves of BN / 2 (of a gated product: of gate and
@@ -587,7 +606,7 @@ __global__ __launch_bounds__(512) void k_few(Work w) {
     if constexpr (EPI == kGated) {
         f32x4_t h;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) h[e] = activation(w.gelu, acc[0][e], nullptr) * acc[1][e];
+        for (int e = 0; e < 4; ++e) h[e] = (w.gelu ? activation<true>(acc[0][e], nullptr) : activation<false>(acc[0][e], nullptr)) * acc[1][e];
         const int64_t to = fr * w.hidden_s + n;
         store4(static_cast<T *>(w.act) + to, h);
         if (w.gate) {
@@ -606,10 +625,10 @@ __global__ __launch_bounds__(256) void k_join_slices(Work w) {
         int which = 0;
         while (which + 1 < w.products && i >= w.p[which + 1].partial) ++which;
         const Product &p = w.p[which];
-        float sum[8], more[8];
-        load8(w.partial + i, sum);
-        for (int s = 1; s < w.slices; ++s) {
-            load8(w.partial + s * w.slice_size + i, more);
+        float sum[8] = {};
+        for (int s = 0; s < w.slices; ++s) {
+            Eight<float> more;
+            more.load(w.partial + s * w.slice_size + i);
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum[e] += more[e];
         }
@@ -701,8 +720,9 @@ hipError_t launch(Work &w, const Plan &plan, float *partial, hipStream_t s) {
     w.slice_size = 0;
     for (int i = 0; i < w.products; ++i) {
         Product &p = w.p[i];
+        p.tiles_m = int(ceil_div(p.m, kSizeOf[plan.kind]));
         p.tiles_n = int(ceil_div(p.n, cols_of(plan.kind, Epilogue(EPI))));
-        p.tiles = int(tiles_of({p.m, p.n}, plan.kind, Epilogue(EPI)));
+        p.tiles = p.tiles_m * p.tiles_n;
         p.partial = w.slice_size;
         w.slice_size += int64_t(p.m) * p.n;
         blocks += int64_t(p.tiles) * plan.slices;

@@ -58,16 +58,19 @@ __device__ inline void store8(float *p, const float *v) {
     reinterpret_cast<f32x4_t *>(p)[0] = a;
     reinterpret_cast<f32x4_t *>(p)[1] = b;
 }
-__device__ inline void load8(const uint16_t *p, float *v) {
-    const bf16x8_t b = *reinterpret_cast<const bf16x8_t *>(p);
+// As they lie in memory, so that many loads fit the registers before any is used.
+template <typename T>
+struct Eight {
+    u32x4_t raw[sizeof(T) / 2];
+    __device__ void load(const T *p) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = float(b[e]);
-}
-__device__ inline void load8(const float *p, float *v) {
-    const f32x4_t a = reinterpret_cast<const f32x4_t *>(p)[0], b = reinterpret_cast<const f32x4_t *>(p)[1];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = a[e], v[e + 4] = b[e];
-}
+        for (int i = 0; i < int(sizeof(T) / 2); ++i) raw[i] = reinterpret_cast<const u32x4_t *>(p)[i];
+    }
+    __device__ float operator[](int e) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(raw[e / 4][e % 4]);
+        else return __uint_as_float(e & 1 ? raw[0][e / 2] & 0xffff0000u : raw[0][e / 2] << 16);
+    }
+};
 // Four of them.
 __device__ inline void store4(uint16_t *p, f32x4_t v) {
     typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
