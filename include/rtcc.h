@@ -685,7 +685,8 @@ RTCC_API rtcc_status rtcc_layer_norm(const rtcc_layer_norm_desc *desc, void *hip
  * the normed tensor, with the same stride.  dweight, dbias: float32 [channels],
  * written, not added to; summed over the rows in a fixed order; NULL: not
  * wanted.  workspace: device memory of at least rtcc_layer_norm_grad_workspace
- * bytes, 16-byte aligned (NULL where that is 0); it needs no initial contents. */
+ * bytes, 16-byte aligned (NULL where that is 0); it needs no initial contents, and
+ * calls that may run at once need one each. */
 typedef struct rtcc_layer_norm_grad_desc {
     rtcc_layer_norm_desc fwd;
     const void *dout, *dsum;
@@ -725,7 +726,8 @@ typedef struct rtcc_gated_ffn_desc {
     int64_t hidden_stride;        /* of gate, up and act                                */
 } rtcc_gated_ffn_desc;
 /* workspace: device memory of at least rtcc_gated_ffn_workspace bytes, 16-byte
- * aligned (NULL where that is 0); it needs no initial contents. */
+ * aligned (NULL where that is 0); it needs no initial contents, and calls that may
+ * run at once need one each. */
 RTCC_API rtcc_status rtcc_gated_ffn_workspace(const rtcc_gated_ffn_desc *desc, size_t *bytes);
 RTCC_API rtcc_status rtcc_gated_ffn(const rtcc_gated_ffn_desc *desc, void *workspace, size_t workspace_bytes,
                                     void *hip_stream);

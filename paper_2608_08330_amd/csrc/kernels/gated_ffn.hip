@@ -4,15 +4,30 @@
 //   dH = dY Wd, dU = dH act(G), dG = dH U act'(G)
 //   dX = dG Wg + dU Wu, dWg = dG' X, dWu = dU' X, dWd = dY' H
 //
-// Every product is a launch of one kernel, k_product, over tiles of its result:
+// Products are tiles of one matrix kernel in three forms: k_product (tiles of 128 or
+// 64, two to five blocks a CU), k_product_large (256, one block a CU that stays) and
+// k_few (up to 16 rows, no tiles).  plan() chooses tiles and slices of the contracted
+// axis by a model of their times.
 //   G and U together: a tile's columns are halves of Wg and of Wu, so a lane has g
 //     and u of the same places in its registers and stores h
-//   dH: the epilogue reads g and u and stores dG and dU
+//   dH: the results read g and u and become dG and dU before they are stored
 //   dX: the contracted axis runs over Wg's rows, then Wu's
 //   dWg, dWu, dWd: up to three products of one launch
 // Operands whose contracted axis is in rows are read transposed from LDS, so no
-// tensor is laid out anew.  bf16 rounds what is stored: H, dG and dU; sums are
-// float32.
+// tensor is laid out anew.
+//
+// bf16 rounds what is stored and then multiplied: h, dG and dU (matrix operands), and
+// g and u where a gradient will read them.  Against 64-bit gradients dX, dWg and dWu
+// are 0.30% off (root mean square; rounding the result alone: 0.17%).  Stored in
+// float32, g and u would leave 0.24%, for 200 MB more traffic in the 290 us of a step
+// over 16,384 rows of 384 channels, 1,536 hidden: some 40 us.  All sums are float32.
+//
+// What bounds them (kernel times of one MI355X): 16,384 rows, 2,048 channels, 8,192
+// hidden: matrix units 53 to 66% busy at 2.0 GHz (the power limit's clock), 1,100 to
+// 1,370 TFLOP/s; the LDS takes 2,560 cycles a step of 256 x 256 x 64 (64 KB written
+// at 64 bytes a cycle, 192 KB read at 128) beside 2,048 of products.  16,384 rows of
+// 384 channels, 1,536 hidden: 290 us a step with 1.0 GB of traffic (200 us at a copy's
+// rate) and contracted axes of six steps, after which a tile's results cost as much.
 #include <algorithm>
 
 #include <hip/hip_runtime.h>
@@ -30,7 +45,7 @@ namespace {
 
 __device__ inline float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// activation(z) = z * gate; *slope = its derivative
+// Activation of z; *slope, where asked for, its derivative.
 __device__ inline float silu(float z, float *slope) {
     const float s = __builtin_amdgcn_rcpf(1.f + exp2_fast(-1.4426950408889634f * z));
     if (slope) *slope = s * fmaf(z, 1.f - s, 1.f);
@@ -92,7 +107,8 @@ enum Epilogue { kPlain, kGated, kGatedGrad };
 
 // The product, the slice and the tile of a block.  Blocks of one XCD (every eighth)
 // take tiles that follow each other, in bands of kBand tiles of rows, so that their
-// operands meet in its L2.
+// operands meet in its L2.  A step over 16,384 rows of 2,048 channels, 8,192 hidden:
+// 3.90 ms in bands of 4, 3.92 of 2, 4.01 of 8, 4.07 of 16.
 struct Spot {
     int which, slice, tile_m, tile_n;  // which < 0: none, past the last one
 };
@@ -212,9 +228,13 @@ __device__ inline void finish(const Work &w, const Product &p, int slice, At at,
 // up).  Four waves, two by two.  STAGES buffers form a ring: the loads run STAGES - 1
 // steps ahead.  A step has two halves, whose fragments have registers of their own:
 // one half's are read while the other's are multiplied.  Reads and loads stand
-// between the products, so that one wave on a SIMD keeps all units busy.
+// between the products, so that one wave on a SIMD keeps all units busy.  The LDS
+// bounds it: 1,024 cycles a step of 128 x 128 x 64 bf16 (32 KB written, 64 KB read)
+// beside 512 of products.  Four buffers for two where a CU has one or two small tiles
+// (64 rows, 2,048 channels, 8,192 hidden: 17 us for 27, 10 for 15.5); elsewhere they
+// change nothing.
 template <typename T, bool AK, bool BK, int EPI, int BM, int BN, int STAGES>
-__global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_product(Work w) {
+__global__ __launch_bounds__(256, 2) void k_product(Work w) {
     constexpr int MT = BM / 32, NT = BN / 64;
     constexpr bool kGate = EPI == kGated, kTwo = EPI == kPlain && AK && !BK;  // kTwo: two segments
     typedef Panel<T, AK, BM> PA;
@@ -338,20 +358,19 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_product(Work w) {
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // no load into LDS outlives the block
 
     // pairs of tiles side by side, or below each other where there is one
-    constexpr int kDown = NT == 1 ? 2 : 1, kAcross = NT == 1 ? 1 : NT / 2;
+    constexpr int kDown = NT == 1 ? 2 : 1;
+    static_assert(NT * kDown == 2, "pairs");
     const int fr = lane & 15, second = (lane >> 4) & 1, col = (lane >> 5) * 8;
-    // unit u: pair j = u % kAcross of half h, rows i
-    constexpr int kHalves = kGate ? 1 : 2, kUnits = MT / kDown * kHalves * kAcross;
+    // unit u: half h = u % kHalves, rows i = u / kHalves * kDown
+    constexpr int kHalves = kGate ? 1 : 2, kUnits = MT / kDown * kHalves;
     auto place = [&](int u) -> Place {
-        const int j = u % kAcross, h = u / kAcross % kHalves, i = u / kAcross / kHalves * kDown;
-        return {m0 + wm * (BM / 2) + 16 * (i + (kDown - 1) * second) + fr,
-                n0 + h * (BN / 2) + wn * (BN / 4) + 32 * j + 16 * (2 - kDown) * second + col};
+        return {m0 + wm * (BM / 2) + 16 * (u / kHalves * kDown + (kDown - 1) * second) + fr,
+                n0 + u % kHalves * (BN / 2) + wn * (BN / 4) + 16 * (NT - 1) * second + col};
     };
     finish<T, EPI, kUnits>(w, p, tile.slice, place, [&](int u, float *c, float *d) {
-        const int j = u % kAcross, h = u / kAcross % kHalves, i = u / kAcross / kHalves * kDown;
-        constexpr int kNext = NT == 1 ? 0 : 1;
-        pair_up(acc[i][h][2 * j], acc[i + kDown - 1][h][2 * j + kNext], c);
-        if (kGate) pair_up(acc[i][1][2 * j], acc[i + kDown - 1][1][2 * j + kNext], d);
+        const int i = u / kHalves * kDown, h = u % kHalves;
+        pair_up(acc[i][h][0], acc[i + kDown - 1][h][NT - 1], c);
+        if (kGate) pair_up(acc[i][1][0], acc[i + kDown - 1][1][NT - 1], d);
     });
 }
 
@@ -369,8 +388,14 @@ __global__ __launch_bounds__(256, BM == 256 ? 1 : 2) void k_product(Work w) {
 // phase p has read is free in phase p + 1; phases 2, 3, 4 and the next 1 fill B0, A0,
 // B1 and A1 with their values of two steps later (in this order all along).  Loads are
 // waited for one phase before they are read, with those of the last five panels
-// still under way.  Blocks stay and take every gridDim.x-th tile;
-// the next tile's first loads are under way while this one's results are stored.
+// still under way.  Blocks stay and take every gridDim.x-th tile; the next tile's
+// first loads are under way while this one's results are stored.
+//
+// Four waves of 128 x 128 would read a third less from LDS; with the pipeline of
+// k_product (512 registers a lane) they took 4.2 ms for 3.9 in a step over 16,384 rows
+// of 2,048 channels, 8,192 hidden.  What is left is the end of a tile, which nothing
+// covers: 7 us of plain results, 12 with g and u stored, 27 of dG and dU (512 KB a
+// tile), beside 1.4 to 1.6 us a step.
 template <bool AK, bool BK, int EPI>
 __global__ __launch_bounds__(512) void k_product_large(Work w) {
     typedef uint16_t T;
@@ -554,7 +579,8 @@ __global__ __launch_bounds__(512) void k_product_large(Work w) {
 // Up to 16 rows: the weights are what is read, once, straight into registers.  A
 // block has COLS (8 or 16) columns of the result; its eight waves share the
 // contracted axis in turns of 128 bytes, kTurns of them under way at a time, and
-// their sums are added up through LDS in the waves' order.
+// their sums are added up through LDS in the waves' order.  One row of 384 channels,
+// 1,536 hidden: 4 + 4 us, most of it the launch; as tiles 5 + 8.
 constexpr int kFewRows = 16;
 template <typename T, int EPI, int COLS>
 __global__ __launch_bounds__(512) void k_few(Work w) {
@@ -658,16 +684,17 @@ int64_t tiles_of(const Size &s, Tiles kind, Epilogue epi) {
     return ceil_div(s.m, kSizeOf[kind]) * ceil_div(s.n, cols_of(kind, epi));
 }
 
-// Microseconds of a launch, by which tiles and slices are chosen.  A CU moves about
-// 58 KB a microsecond into LDS, whatever the tile (bf16; 128: 32 KB a step, 0.5 us, or
-// 0.62 us for a block that has the CU to itself; 256: 64 KB in 1.4 us, all CUs being
-// busy), so that large tiles win where they fill the device and little of their time
-// goes into first loads and stores, which nothing covers there.  float32 is bound by
-// its products.  Measured against it (plain results, kernel times): 16,384 x 384, K
-// 1,536: 128 32 us (modelled 32), 256 42 (46), 64 39; 32,768 x 384: 256 46 (46), 128
-// 48 (50); three products of 1,536 x 384, K 16,384: 256 in 7 slices 68 + 10 (78), 128
-// in 4 72 + 7 (81), 64 in 4 113 + 7; 500 x 1,024, K 2,816: 64 in 4 slices 13 + 4 (19),
-// whole 23 (26), 128 whole 33 (35).
+// Microseconds of a launch, by which tiles and slices are chosen.  A step takes the
+// time of its LDS traffic, some 58 KB loaded a microsecond and CU whatever the tile
+// (bf16; 128: 32 KB, 0.5 us, or 0.62 us for a block that has the CU to itself; 256: 64
+// KB in 1.4 us, all CUs being busy at a lower clock), so that large tiles win where
+// they fill the device and little of their time goes into first loads and results,
+// which nothing covers there.  float32 is bound by its products.  Measured against it
+// (plain results, kernel times): 16,384 x 384, K 1,536: 128 32 us (modelled 32), 256
+// 42 (46), 64 39; 32,768 x 384: 256 44 (46), 128 48 (50); three products of 1,536 x
+// 384, K 16,384: 256 in 7 slices 72 + 10 (80), 128 in 4 70 + 7 (84), 64 in 4 113 + 7;
+// 500 x 1,024, K 2,816: 64 with four buffers 12 (18), in 4 slices 11 + 5, 64 with two
+// 23 (26), 128 33 (35).
 struct Cost {
     int resident;                              // blocks of a CU
     double alone, shared;                      // a step of one block, and of each of several

@@ -158,9 +158,8 @@ struct Panel {
     // Fills the panel with THREADS threads, 16 bytes each a load, step after step.
     // What lies past the operand becomes zero: the hardware returns zero beyond the
     // buffer's length, and lanes past the end of a line get an offset beyond it.
-    // The state but off and chunk is wave-uniform and stays in scalar registers; a
-    // step costs a few scalar instructions a panel (88 a step, with what a step's
-    // addresses were computed anew, took as long as the step's products).
+    // The state but off and chunk is wave-uniform; a step costs a few scalar
+    // instructions a panel.
     template <int THREADS>
     struct Feed {
         static constexpr int kLoads = kLines * kChunks / THREADS;
