@@ -12,7 +12,7 @@
 //     and u of the same places in its registers and stores h
 //   dH: the results read g and u and become dG and dU before they are stored
 //   dX: the contracted axis runs over Wg's rows, then Wu's
-//   dWg, dWu, dWd: up to three products of one launch
+//   dWg, dWu, dWd: up to three products of one launch, which may be dX's
 // Operands whose contracted axis is in rows are read transposed from LDS, so no
 // tensor is laid out anew.
 //
@@ -233,9 +233,12 @@ __device__ inline void finish(const Work &w, const Product &p, int slice, At at,
 // beside 512 of products.  Four buffers for two where a CU has one or two small tiles
 // (64 rows, 2,048 channels, 8,192 hidden: 17 us for 27, 10 for 15.5); elsewhere they
 // change nothing.
-template <typename T, bool AK, bool BK, int EPI, int BM, int BN, int STAGES>
-__global__ __launch_bounds__(256, 2) void k_product(Work w) {
-    constexpr int MT = BM / 32, NT = BN / 64;
+template <typename T, int BM, int STAGES>
+constexpr uint32_t kProductLds = STAGES * 2 * BM * 128;  // a step is 128 bytes, tiles are square
+
+template <typename T, bool AK, bool BK, int EPI, int BM, int STAGES>
+__device__ inline void product(const Work &w, uint32_t id, char *lds) {
+    constexpr int BN = BM, MT = BM / 32, NT = BN / 64;
     constexpr bool kGate = EPI == kGated, kTwo = EPI == kPlain && AK && !BK;  // kTwo: two segments
     typedef Panel<T, AK, BM> PA;
     typedef Panel<T, BK, BN / 2> PB;
@@ -243,11 +246,11 @@ __global__ __launch_bounds__(256, 2) void k_product(Work w) {
     typedef typename PB::template Feed<256> FB;
     constexpr uint32_t kStage = PA::kBytes + 2 * PB::kBytes;
     constexpr int kLoads = FA::kLoads + 2 * FB::kLoads, kStep = PA::kStep;
-    __shared__ __attribute__((aligned(1024))) char lds[STAGES * kStage];
+    static_assert(STAGES * kStage == kProductLds<T, BM, STAGES>, "LDS of a block");
 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wm = wave >> 1, wn = wave & 1;
-    const Spot tile = spot(w, blockIdx.z * gridDim.x + blockIdx.x);
+    const Spot tile = spot(w, id);
     if (tile.which < 0) return;
     const Product p = pick(w, tile.which);
     const int m0 = tile.tile_m * BM, n0 = tile.tile_n * (kGate ? BN / 2 : BN);
@@ -372,6 +375,24 @@ __global__ __launch_bounds__(256, 2) void k_product(Work w) {
         pair_up(acc[i][h][0], acc[i + kDown - 1][h][NT - 1], c);
         if (kGate) pair_up(acc[i][1][0], acc[i + kDown - 1][1][NT - 1], d);
     });
+}
+
+template <typename T, bool AK, bool BK, int EPI, int BM, int STAGES>
+__global__ __launch_bounds__(256, 2) void k_product(Work w) {
+    __shared__ __attribute__((aligned(1024))) char lds[kProductLds<T, BM, STAGES>];
+    product<T, AK, BK, EPI, BM, STAGES>(w, blockIdx.z * gridDim.x + blockIdx.x, lds);
+}
+
+// dX and the weights' gradients, neither of which needs the other's, in one launch;
+// first: blocks of those with more steps, which start first (x_first: dX's).
+template <typename T, int BM, int STAGES>
+__global__ __launch_bounds__(256, 2) void k_products(Work x, Work w, uint32_t first, bool x_first) {
+    __shared__ __attribute__((aligned(1024))) char lds[kProductLds<T, BM, STAGES>];
+    uint32_t id = blockIdx.z * gridDim.x + blockIdx.x;
+    const bool early = id < first;
+    id = early ? id : id - first;
+    if (early == x_first) product<T, true, false, kPlain, BM, STAGES>(x, id, lds);
+    else product<T, false, false, kPlain, BM, STAGES>(w, id, lds);
 }
 
 // bf16, tiles of 256 x 256, eight waves of 128 x 64: rows 64 wm .. of both halves of
@@ -671,6 +692,7 @@ struct Plan {
     Tiles kind;
     int slices, per_slice, steps;
     size_t partial;  // bytes
+    double us;       // modelled
 };
 constexpr int kSizeOf[] = {256, 128, 64, 64};
 struct Size {
@@ -729,7 +751,7 @@ Plan plan(const Size *sizes, int count, bool bf16, int64_t k, int segments, Epil
             if (slices > 1) t += kJoin + double(values) * slices * 4 * kJoinByte;
             if (least == 0 || t < least) {
                 least = t;
-                best = Plan{kind, int(slices), int(each), int(steps), 0};
+                best = Plan{kind, int(slices), int(each), int(steps), 0, t};
             }
         }
     }
@@ -738,9 +760,9 @@ Plan plan(const Size *sizes, int count, bool bf16, int64_t k, int segments, Epil
     return best;
 }
 
-template <typename T, bool AK, bool BK, int EPI>
-hipError_t launch(Work &w, const Plan &plan, float *partial, hipStream_t s) {
-    int64_t blocks = 0;
+// Fills in the tiles of w's products; the number of blocks.
+int64_t cut(Work &w, const Plan &plan, Epilogue epi, float *partial) {
+    int64_t tiles = 0;
     w.slices = plan.slices;
     w.per_slice = plan.per_slice;
     w.partial = partial;
@@ -748,26 +770,56 @@ hipError_t launch(Work &w, const Plan &plan, float *partial, hipStream_t s) {
     for (int i = 0; i < w.products; ++i) {
         Product &p = w.p[i];
         p.tiles_m = int(ceil_div(p.m, kSizeOf[plan.kind]));
-        p.tiles_n = int(ceil_div(p.n, cols_of(plan.kind, Epilogue(EPI))));
+        p.tiles_n = int(ceil_div(p.n, cols_of(plan.kind, epi)));
         p.tiles = p.tiles_m * p.tiles_n;
         p.partial = w.slice_size;
         w.slice_size += int64_t(p.m) * p.n;
-        blocks += int64_t(p.tiles) * plan.slices;
+        tiles += p.tiles;
     }
+    return tiles * plan.slices;
+}
+
+template <typename T>
+hipError_t join(const Work &w, hipStream_t s) {
+    if (w.slices == 1) return hipSuccess;
+    k_join_slices<T><<<int(std::min<int64_t>((w.slice_size + 2047) / 2048, 8 * compute_units())), 256, 0, s>>>(w);
+    return hipGetLastError();
+}
+
+template <typename T, bool AK, bool BK, int EPI>
+hipError_t launch(Work &w, const Plan &plan, float *partial, hipStream_t s) {
+    const int64_t blocks = cut(w, plan, Epilogue(EPI), partial);
     const Fold f = fold(blocks, 256);
     const dim3 grid(f.x, 1, f.z);
     switch (plan.kind) {
         case kTiles256:
-            if constexpr (sizeof(T) == 2) k_product_large<AK, BK, EPI><<<int(std::min<int64_t>(blocks, compute_units())), 512, 0, s>>>(w);
+            if constexpr (sizeof(T) == 2)
+                k_product_large<AK, BK, EPI><<<int(std::min<int64_t>(blocks, compute_units())), 512, 0, s>>>(w);
             break;
-        case kTiles128: k_product<T, AK, BK, EPI, 128, 128, 2><<<grid, 256, 0, s>>>(w); break;
-        case kTiles64Deep: k_product<T, AK, BK, EPI, 64, 64, 4><<<grid, 256, 0, s>>>(w); break;
-        case kTiles64: k_product<T, AK, BK, EPI, 64, 64, 2><<<grid, 256, 0, s>>>(w); break;
+        case kTiles128: k_product<T, AK, BK, EPI, 128, 2><<<grid, 256, 0, s>>>(w); break;
+        case kTiles64: k_product<T, AK, BK, EPI, 64, 2><<<grid, 256, 0, s>>>(w); break;
+        case kTiles64Deep: k_product<T, AK, BK, EPI, 64, 4><<<grid, 256, 0, s>>>(w); break;
+    }
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess ? e : join<T>(w, s);
+}
+
+// x and w in one launch, of one kind of tiles (not the largest).
+template <typename T>
+hipError_t launch_both(Work &x, const Plan &px, float *partial_x, Work &w, const Plan &pw, float *partial_w, hipStream_t s) {
+    const int64_t blocks_x = cut(x, px, kPlain, partial_x), blocks_w = cut(w, pw, kPlain, partial_w);
+    const bool x_first = px.per_slice >= pw.per_slice;
+    const uint32_t first = uint32_t(x_first ? blocks_x : blocks_w);
+    const Fold f = fold(blocks_x + blocks_w, 256);
+    const dim3 grid(f.x, 1, f.z);
+    switch (px.kind) {
+        case kTiles128: k_products<T, 128, 2><<<grid, 256, 0, s>>>(x, w, first, x_first); break;
+        case kTiles64: k_products<T, 64, 2><<<grid, 256, 0, s>>>(x, w, first, x_first); break;
+        default: k_products<T, 64, 4><<<grid, 256, 0, s>>>(x, w, first, x_first); break;
     }
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || plan.slices == 1) return e;
-    k_join_slices<T><<<int(std::min<int64_t>((w.slice_size + 2047) / 2048, 8 * compute_units())), 256, 0, s>>>(w);
-    return hipGetLastError();
+    if (e == hipSuccess) e = join<T>(x, s);
+    return e != hipSuccess ? e : join<T>(w, s);
 }
 
 // Eight columns a block where sixteen would leave CUs without one.
@@ -793,17 +845,63 @@ Plan plan_dhidden(const FfnArgs &a) {
     const Size s{a.rows, a.hidden};
     return plan(&s, 1, a.bf16, a.channels, 1, kGatedGrad, true, false);
 }
-Plan plan_dx(const FfnArgs &a) {
-    const Size s{a.rows, a.channels};
-    return plan(&s, 1, a.bf16, a.hidden, 2, kPlain, a.w_gate_s == a.w_up_s, false);
-}
-Plan plan_weights(const FfnArgs &a) {
-    Size s[kMaxProducts];
+// dX and the weights' gradients: plans of their own launches, or of one for both.
+struct Backward {
+    bool both;
+    Plan x, w;
+    size_t partial;  // bytes
+};
+Backward plan_backward(const FfnArgs &a) {
+    Size x{a.rows, a.channels}, s[kMaxProducts];
     int n = 0;
     if (a.dw_gate) s[n++] = {a.hidden, a.channels};
     if (a.dw_up) s[n++] = {a.hidden, a.channels};
     if (a.dw_down) s[n++] = {a.channels, a.hidden};
-    return plan(s, n, a.bf16, a.rows, 1, kPlain, true, false);
+    const bool dx = a.dx && a.rows > 0;
+    Backward b{};
+    if (dx) b.x = plan(&x, 1, a.bf16, a.hidden, 2, kPlain, a.w_gate_s == a.w_up_s, false);
+    if (n) b.w = plan(s, n, a.bf16, a.rows, 1, kPlain, true, false);
+    b.partial = std::max(b.x.partial, b.w.partial);
+    if (!dx || !n) return b;
+    // One launch: the steps of both over all CUs, or those of a longest block, at the
+    // pace of a full CU while there are others' steps beside it and then of its own.
+    // 500 rows, 1,024 channels, 2,816 hidden: 26 + 5 us for 14 + 5 + 21; 16,384 rows,
+    // 384, 1,536: 112 + 8 for 51 + 72 + 10 (173 where longer blocks came last).
+    double least = b.x.us + b.w.us;
+    const int64_t cus = compute_units(), wide = a.bf16 ? 64 : 32;
+    const int64_t steps_x = 2 * ceil_div(a.hidden, wide), steps_w = ceil_div(a.rows, wide);
+    int64_t values_w = 0;
+    for (int i = 0; i < n; ++i) values_w += s[i].m * s[i].n;
+    const int64_t values_x = x.m * x.n;
+    for (Tiles kind : {kTiles128, kTiles64, kTiles64Deep}) {
+        const Cost &c = kCost[a.bf16][kind];
+        const int64_t tiles_x = tiles_of(x, kind, kPlain);
+        int64_t tiles_w = 0;
+        for (int i = 0; i < n; ++i) tiles_w += tiles_of(s[i], kind, kPlain);
+        for (int64_t sx = 1; sx <= 16 && (sx == 1 || (sx * 4 <= steps_x && tiles_x <= 4 * cus)); sx *= 2)
+            for (int64_t sw = 1; sw <= 16 && (sw == 1 || (sw * 4 <= steps_w && tiles_w <= 4 * cus)); sw *= 2) {
+                const int64_t each_x = ceil_div(steps_x, sx), each_w = ceil_div(steps_w, sw);
+                const int64_t blocks = ceil_div(tiles_x * sx + tiles_w * sw, cus);
+                const double all = double(tiles_x * sx * each_x + tiles_w * sw * each_w) / double(cus);
+                const double longest = double(std::max(each_x, each_w)), beside = std::max(0.0, all - longest);
+                const double together = std::min(longest, beside / (c.resident - 1));
+                const double path = together * std::max(c.alone, c.resident * c.shared) + (longest - together) * c.alone;
+                double t = kLaunch + double(ceil_div(blocks, c.resident)) * c.plain + std::max(all * c.shared, path);
+                if (sx > 1) t += kJoin + double(values_x) * sx * 4 * kJoinByte;
+                if (sw > 1) t += kJoin + double(values_w) * sw * 4 * kJoinByte;
+                if (t >= least) continue;
+                least = t;
+                b.both = true;
+                b.x = Plan{kind, int(ceil_div(steps_x, each_x)), int(each_x), int(steps_x), 0, t};
+                b.w = Plan{kind, int(ceil_div(steps_w, each_w)), int(each_w), int(steps_w), 0, t};
+            }
+    }
+    if (b.both) {
+        b.x.partial = b.x.slices > 1 ? size_t(values_x) * b.x.slices * sizeof(float) : 0;
+        b.w.partial = b.w.slices > 1 ? size_t(values_w) * b.w.slices * sizeof(float) : 0;
+        b.partial = b.x.partial + b.w.partial;  // multiples of 32 bytes
+    }
+    return b;
 }
 
 bool wants_hidden(const FfnArgs &a) { return a.dx || a.dw_gate || a.dw_up; }
@@ -860,19 +958,18 @@ hipError_t gradient(const FfnArgs &a, hipStream_t s) {
         p.c = dgate;
         if ((e = launch<T, true, false, kGatedGrad>(w, plan_dhidden(a), nullptr, s)) != hipSuccess) return e;
     }
+    const Backward plans = plan_backward(a);
+    Work x{}, w{};
     if (a.rows > 0 && a.dx) {
-        Work w{};
-        w.products = 1;
-        Product &p = w.p[0];
+        x.products = 1;
+        Product &p = x.p[0];
         p.a[0] = dgate, p.a[1] = dup;
         p.b[0] = static_cast<const char *>(a.w_gate), p.b[1] = static_cast<const char *>(a.w_up);
         p.a_row = hidden_row;
         p.b_row[0] = uint32_t(a.w_gate_s * sizeof(T)), p.b_row[1] = uint32_t(a.w_up_s * sizeof(T));
         p.m = a.rows, p.n = a.channels, p.k = a.hidden;
         p.c = a.dx, p.c_row = a.dx_s;
-        if ((e = launch<T, true, false, kPlain>(w, plan_dx(a), partial, s)) != hipSuccess) return e;
     }
-    Work w{};
     auto add = [&](void *c, int64_t c_row, const void *from, uint32_t from_row, const void *with, uint32_t with_row, int m, int n) {
         if (!c) return;
         Product &p = w.p[w.products++];
@@ -885,8 +982,10 @@ hipError_t gradient(const FfnArgs &a, hipStream_t s) {
     add(a.dw_gate, a.dw_gate_s, dgate, hidden_row, a.x, x_row, a.hidden, a.channels);
     add(a.dw_up, a.dw_up_s, dup, hidden_row, a.x, x_row, a.hidden, a.channels);
     add(a.dw_down, a.dw_down_s, a.dout, dout_row, a.act, saved_row, a.channels, a.hidden);
-    if (!w.products) return hipSuccess;
-    return launch<T, false, false, kPlain>(w, plan_weights(a), partial, s);
+    if (plans.both)
+        return launch_both<T>(x, plans.x, partial, w, plans.w, partial + plans.x.partial / sizeof(float), s);
+    if (x.products && (e = launch<T, true, false, kPlain>(x, plans.x, partial, s)) != hipSuccess) return e;
+    return w.products ? launch<T, false, false, kPlain>(w, plans.w, partial, s) : hipSuccess;
 }
 
 }  // namespace
@@ -903,9 +1002,7 @@ int gated_ffn(const FfnArgs &a, void *stream) {
 
 size_t gated_ffn_grad_workspace(const FfnArgs &a) {
     const size_t hidden = wants_hidden(a) ? round16(2 * hidden_bytes(a)) : 0;
-    const size_t dx = a.dx && a.rows ? plan_dx(a).partial : 0;
-    const size_t weights = a.dw_gate || a.dw_up || a.dw_down ? plan_weights(a).partial : 0;
-    return hidden + std::max(dx, weights);
+    return hidden + plan_backward(a).partial;
 }
 
 int gated_ffn_grad(const FfnArgs &a, void *stream) {
