@@ -185,8 +185,8 @@ template <typename T, int G, int V, bool PAST>
 __global__ __launch_bounds__(kThreads<G>, 2) void k_layer_norm_grad(LayerNormArgs a) {
     constexpr int kRows = kThreads<G> / G;
     constexpr int kTensors = PAST ? 3 : 2;
-    // two rows of float32 in four eights a channel would not fit the registers
-    constexpr bool kAhead = sizeof(T) == 2 || V * kTensors <= 8;
+    // what fits the registers
+    constexpr bool kAhead = sizeof(T) == 2 ? V <= 3 : V * kTensors <= 6;
     __shared__ float part[3][G > 64 ? G / 64 : 1][2];
     const int l = threadIdx.x % G;
     const float over = 1.f / float(a.channels);
@@ -216,7 +216,11 @@ __global__ __launch_bounds__(kThreads<G>, 2) void k_layer_norm_grad(LayerNormArg
     const int64_t ahead = int64_t(gridDim.x) * kRows;
     if (kAhead && row < a.rows) fetch(row);
     for (; row < a.rows; row += ahead) {
-        if (!kAhead) fetch(row);
+        if (!kAhead) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) x[v] = dy[v] = ds[v] = Eight<T>{};  // not kept over the row
+            fetch(row);
+        }
         // channels past the end hold zeros
         float n[V][8], y[V][8], past[V][8], sum[1] = {}, square[1] = {}, dots[2] = {};
 #pragma unroll
@@ -324,29 +328,38 @@ __global__ __launch_bounds__(kSumChannels *kSumThreads) void k_layer_norm_sums(L
     }
 }
 
-// Threads of a row and eights of channels each: the fewest threads that hold the
-// row in at most four.
+// Threads of a row and eights of channels each: the fewest threads that hold the row
+// in at most `most` eights, or, of the longest rows, in four.
 struct Cut {
     int g, v;
 };
-Cut cut(int channels) {
+Cut cut(int channels, int most) {
     const int eights = channels / 8;
     for (int g : {8, 16, 32, 64, 256, 512})
-        if (eights <= 4 * g) return {g, (eights + g - 1) / g};
-    return {512, 4};  // not reached: channels <= 16384
+        if (eights <= most * g) return {g, (eights + g - 1) / g};
+    return {512, (eights + 511) / 512};
 }
+// Three eights, of float32 with a gradient past the norm two: then the next row's fit
+// the registers beside this one's and the sums (2,281 rows of 7,712 channels, bf16, 512
+// threads with two: 40 us, 256 with four 86; 16,384 of 2,048: 56 us, 64 threads with
+// four 99).
+Cut grad_cut(const LayerNormArgs &a) { return cut(a.channels, !a.bf16 && a.residual ? 2 : 3); }
 
-// Two blocks a CU: as many as fit it, and their sums stay small.
+// Two blocks a CU, one of 512 threads: as many as fit it, and their sums stay small.
 int grad_blocks(const LayerNormArgs &a) {
-    const int per = std::max(1, 256 / cut(a.channels).g);
-    return int(std::min<int64_t>(row_tiles(a.rows, per), 2 * compute_units()));
+    const Cut c = grad_cut(a);
+    return int(std::min<int64_t>(row_tiles(a.rows, std::max(1, 256 / c.g)), (c.g > 256 ? 1 : 2) * compute_units()));
 }
 
 template <typename T, int G, int V>
 hipError_t run(const LayerNormArgs &a, int grad_blocks, hipStream_t s) {
     if (grad_blocks) {
-        if (a.residual) k_layer_norm_grad<T, G, V, true><<<grad_blocks, kThreads<G>, 0, s>>>(a);
-        else k_layer_norm_grad<T, G, V, false><<<grad_blocks, kThreads<G>, 0, s>>>(a);
+        // of what grad_cut() gives
+        constexpr bool kPast = G == 512 || V <= (sizeof(T) == 4 ? 2 : 3), kAlone = G == 512 || V <= 3;
+        if constexpr (kPast)
+            if (a.residual) k_layer_norm_grad<T, G, V, true><<<grad_blocks, kThreads<G>, 0, s>>>(a);
+        if constexpr (kAlone)
+            if (!a.residual) k_layer_norm_grad<T, G, V, false><<<grad_blocks, kThreads<G>, 0, s>>>(a);
     } else {
         const Fold f = fold(row_tiles(a.rows, kThreads<G> / G), kThreads<G>);
         k_layer_norm<T, G, V><<<dim3(f.x, 1, f.z), kThreads<G>, 0, s>>>(a);
@@ -366,7 +379,7 @@ hipError_t run(const LayerNormArgs &a, int v, int grad_blocks, hipStream_t s) {
 
 template <typename T>
 hipError_t run(const LayerNormArgs &a, int grad_blocks, hipStream_t s) {
-    const Cut c = cut(a.channels);
+    const Cut c = grad_blocks ? grad_cut(a) : cut(a.channels, 4);
     switch (c.g) {
         case 8: return run<T, 8>(a, c.v, grad_blocks, s);
         case 16: return run<T, 16>(a, c.v, grad_blocks, s);
