@@ -535,6 +535,70 @@ def test_a_step_in_a_graph_and_on_a_stream(precision, rows):
             assert all(torch.equal(a, b) for a, b in zip(results[0], other))
 
 
+@pytest.mark.parametrize("precision", PRECISIONS)
+def test_rows_as_far_apart_as_they_may_be(precision):
+    """2^22 elements between rows: a tile's rows span up to 2^31 bytes."""
+    import torch
+    c = Unit(precision, 130, 72, 40, True)
+
+    def apart(t):
+        wide = torch.empty((t.shape[0] - 1) * (1 << 22) + t.shape[1], dtype=t.dtype, device="cuda")
+        far = wide.as_strided(t.shape, (1 << 22, 1))
+        far.copy_(t)
+        return far
+
+    x, out, gate, up, act = (apart(t.x) for t in (c.gx, c.out, *c.saved))
+    wg, wu, wd = (apart(t) for t in (c.gwg, c.gwu, c.gwd.x))
+    d = R.gated_ffn_desc(x, wg, wu, wd, out, R.RTCC_ACT_GELU, gate, up, act)
+    n = R.rtcc_gated_ffn_workspace(d)
+    space = _space(n)
+    R.rtcc_gated_ffn(d, space.data_ptr(), n)
+    torch.cuda.synchronize()
+    for to, t in zip([c.out] + c.saved, (out, gate, up, act)):
+        to.x.copy_(t)
+    c.check()
+    c.gradients()
+    near = [t.x.clone() for t in c.grads]
+    far = [apart(t) for t in (c.gx.x, c.gwg, c.gwu, c.gwd.x)]
+    g = R.gated_ffn_grad_desc(d, apart(c.gdy.x), *far)
+    n = R.rtcc_gated_ffn_grad_workspace(g)
+    space = _space(n)
+    R.rtcc_gated_ffn_grad(g, space.data_ptr(), n)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(near, far))
+    norm = Norm(precision, 130, 72)
+    near, total = norm.guarded(), norm.guarded()
+    R.rtcc_layer_norm(norm.desc(near.x, total.x))
+    x, r, out = apart(norm.gx.x), apart(norm.gr.x), apart(near.x)
+    R.rtcc_layer_norm(R.layer_norm_desc(x, out, norm.gw, norm.gb, residual=r, sum_out=x, eps=norm.eps))
+    torch.cuda.synchronize()
+    assert torch.equal(out, near.x) and torch.equal(x, total.x)
+
+
+@pytest.mark.parametrize("precision", PRECISIONS)
+def test_two_streams_at_once(precision):
+    """Units of their own workspaces on two streams: what each gives alone."""
+    import torch
+    units = [Unit(precision, rows, 264, 520, rows > 100, seed=rows).forward().gradients() for rows in (40, 900)]
+    alone = [[t.x.clone() for t in [c.out] + c.saved + c.grads] for c in units]
+    calls = []
+    for c in units:
+        d = c.desc()
+        g = R.gated_ffn_grad_desc(d, c.gdy.x, *(t.x for t in c.grads))
+        n, m = R.rtcc_gated_ffn_workspace(d), R.rtcc_gated_ffn_grad_workspace(g)
+        calls.append((d, _space(n), n, g, _space(m), m, torch.cuda.Stream()))
+        for t in [c.out] + c.saved + c.grads:
+            t.x.fill_(float("nan"))
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for d, sd, n, g, sg, m, stream in calls:
+            R.rtcc_gated_ffn(d, sd.data_ptr(), n, stream.cuda_stream)
+            R.rtcc_gated_ffn_grad(g, sg.data_ptr(), m, stream.cuda_stream)
+    torch.cuda.synchronize()
+    for c, want in zip(units, alone):
+        assert all(torch.equal(t.x, w) for t, w in zip([c.out] + c.saved + c.grads, want))
+
+
 def test_rows_past_32_bits():
     """Outputs and stored values of more than 2^31 elements (4.3 GB a tensor)."""
     import torch
