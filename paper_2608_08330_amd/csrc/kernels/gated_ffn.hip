@@ -12,21 +12,22 @@
 //     and u of the same places in its registers and stores h
 //   dH: the results read g and u and become dG and dU before they are stored
 //   dX: the contracted axis runs over Wg's rows, then Wu's
-//   dWg, dWu, dWd: up to three products of one launch, which may be dX's
+//   dWg, dWu, dWd: up to three products of one launch, which may hold dX's too
+//     (k_products)
 // Operands whose contracted axis is in rows are read transposed from LDS, so no
 // tensor is laid out anew.
 //
 // bf16 rounds what is stored and then multiplied: h, dG and dU (matrix operands), and
 // g and u where a gradient will read them.  Against 64-bit gradients dX, dWg and dWu
 // are 0.30% off (root mean square; rounding the result alone: 0.17%).  Stored in
-// float32, g and u would leave 0.24%, for 200 MB more traffic in the 290 us of a step
+// float32, g and u would leave 0.24%, for 200 MB more traffic in the 270 us of a step
 // over 16,384 rows of 384 channels, 1,536 hidden: some 40 us.  All sums are float32.
 //
 // What bounds them (kernel times of one MI355X): 16,384 rows, 2,048 channels, 8,192
 // hidden: matrix units 53 to 66% busy at 2.0 GHz (the power limit's clock), 1,100 to
 // 1,370 TFLOP/s; the LDS takes 2,560 cycles a step of 256 x 256 x 64 (64 KB written
 // at 64 bytes a cycle, 192 KB read at 128) beside 2,048 of products.  16,384 rows of
-// 384 channels, 1,536 hidden: 290 us a step with 1.0 GB of traffic (200 us at a copy's
+// 384 channels, 1,536 hidden: 270 us a step with 1.0 GB of traffic (200 us at a copy's
 // rate) and contracted axes of six steps, after which a tile's results cost as much.
 #include <algorithm>
 
