@@ -712,7 +712,10 @@ typedef enum rtcc_activation {
  * gate, up, act: [rows][hidden] of one stride, what the gradients read of the
  * forward call (g, u and h); all of them or none.  Without them h is held in the
  * workspace.  bf16: h is rounded to bf16 for the product with w_down; g and u
- * are rounded only where they are stored. */
+ * are rounded only where they are stored.  out may be x, with the same stride;
+ * out, gate, up and act overlap neither one another nor the other tensors of the
+ * call, the workspace overlaps none.  An overlap that would change results is
+ * refused (RTCC_E_ARG). */
 typedef struct rtcc_gated_ffn_desc {
     int32_t abi_version;          /* RTCC_ABI_VERSION                                   */
     int32_t precision;            /* rtcc_precision of all tensors                      */
@@ -736,7 +739,10 @@ RTCC_API rtcc_status rtcc_gated_ffn(const rtcc_gated_ffn_desc *desc, void *works
  * the forward call, whose gate, up and act (required) are read as they were
  * rounded; its out is ignored.  dout: as out.  dx, dw_gate, dw_up, dw_down: as
  * x and the weights; written, not added to (no rows: the weights' are 0); NULL:
- * not wanted.  Every sum is in a fixed order: the results of two calls are the
+ * not wanted.  They overlap neither one another nor the tensors that are read, the
+ * workspace overlaps none: an overlap that would change results is refused
+ * (RTCC_E_ARG), as that of dx with x or dout where the weights' gradients read
+ * these.  Every sum is in a fixed order: the results of two calls are the
  * same bits.  bf16: the gradients of g and u are rounded to bf16 for the
  * products with the weights and with x. */
 typedef struct rtcc_gated_ffn_grad_desc {

@@ -191,6 +191,8 @@ size_t gated_ffn_workspace(const FfnArgs &) { return 0; }
 int gated_ffn(const FfnArgs &, void *) { return -1; }
 size_t gated_ffn_grad_workspace(const FfnArgs &) { return 0; }
 int gated_ffn_grad(const FfnArgs &, void *) { return -1; }
+std::string gated_ffn_overlap(const FfnArgs &) { return {}; }  // no launches that could disagree
+std::string gated_ffn_grad_overlap(const FfnArgs &) { return {}; }
 const char *launch_error(int) { return nullptr; }
 }  // namespace kern
 }  // namespace rtcc

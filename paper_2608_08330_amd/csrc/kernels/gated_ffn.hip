@@ -30,10 +30,13 @@
 // 384 channels, 1,536 hidden: 270 us a step with 1.0 GB of traffic (200 us at a copy's
 // rate) and contracted axes of six steps, after which a tile's results cost as much.
 #include <algorithm>
+#include <initializer_list>
+#include <string>
 
 #include <hip/hip_runtime.h>
 
 #include "compute_units.hpp"
+#include "matrix_overlap.hpp"
 #include "products.hpp"
 #include "token_ops.hpp"
 
@@ -989,7 +992,52 @@ hipError_t gradient(const FfnArgs &a, hipStream_t s) {
     return w.products ? launch<T, false, false, kPlain>(w, plans.w, partial, s) : hipSuccess;
 }
 
+// Tensors of a call that may not share memory.
+struct Named {
+    const char *name;
+    Extent e;
+};
+// First of `some` and `others` that do.
+std::string together(std::initializer_list<Named> some, std::initializer_list<Named> others) {
+    for (const Named &s : some)
+        for (const Named &o : others)
+            if (overlap(s.e, o.e)) return std::string(s.name) + " overlaps " + o.name;
+    return {};
+}
+
 }  // namespace
+
+// The first product reads x, w_gate and w_up and writes gate, up and act; the second
+// reads act and w_down and writes out.  So out may lie where x is.
+std::string gated_ffn_overlap(const FfnArgs &a) {
+    const int64_t n = a.rows, c = a.channels, f = a.hidden, el = a.bf16 ? 2 : 4;
+    const Named x{"x", extent(a.x, n, a.x_s, c, el)}, out{"out", extent(a.out, n, a.out_s, c, el)};
+    const Named wg{"w_gate", extent(a.w_gate, n ? f : 0, a.w_gate_s, c, el)}, wu{"w_up", extent(a.w_up, n ? f : 0, a.w_up_s, c, el)};
+    const Named wd{"w_down", extent(a.w_down, n ? c : 0, a.w_down_s, f, el)};
+    const Named g{"gate", extent(a.gate, n, a.hidden_s, f, el)}, u{"up", extent(a.up, n, a.hidden_s, f, el)};
+    const Named h{"act", extent(a.act, n, a.hidden_s, f, el)};
+    std::string why = together({g, u, h}, {x, wg, wu, wd, out});
+    if (why.empty()) why = together({g}, {u, h});
+    if (why.empty()) why = together({u}, {h});
+    return why.empty() ? together({out}, {wd}) : why;
+}
+
+// dX reads w_gate and w_up, the weights' gradients x, dout and act, in one launch or
+// in two in either order.
+std::string gated_ffn_grad_overlap(const FfnArgs &a) {
+    const int64_t n = a.rows, c = a.channels, f = a.hidden, el = a.bf16 ? 2 : 4;
+    const bool of_x = a.dw_gate || a.dw_up, of_act = a.dw_down, of_weights = a.dx && n;
+    const Named dx{"dx", extent(a.dx, n, a.dx_s, c, el)}, dg{"dw_gate", extent(a.dw_gate, f, a.dw_gate_s, c, el)};
+    const Named du{"dw_up", extent(a.dw_up, f, a.dw_up_s, c, el)}, dd{"dw_down", extent(a.dw_down, c, a.dw_down_s, f, el)};
+    const Named x{"x", extent(a.x, of_x ? n : 0, a.x_s, c, el)}, dout{"dout", extent(a.dout, of_act ? n : 0, a.dout_s, c, el)};
+    const Named h{"act", extent(a.act, of_act ? n : 0, a.hidden_s, f, el)};
+    const Named wg{"w_gate", extent(a.w_gate, of_weights ? f : 0, a.w_gate_s, c, el)};
+    const Named wu{"w_up", extent(a.w_up, of_weights ? f : 0, a.w_up_s, c, el)};
+    std::string why = together({dx, dg, du, dd}, {x, dout, h, wg, wu});
+    if (why.empty()) why = together({dx}, {dg, du, dd});
+    if (why.empty()) why = together({dg}, {du, dd});
+    return why.empty() ? together({du}, {dd}) : why;
+}
 
 size_t gated_ffn_workspace(const FfnArgs &a) {
     if (a.rows == 0) return 0;

@@ -8,6 +8,7 @@
 #include <algorithm>
 #include <cstddef>
 #include <cstdint>
+#include <string>
 
 namespace rtcc {
 namespace kern {
@@ -120,6 +121,9 @@ size_t gated_ffn_workspace(const FfnArgs &a);
 int gated_ffn(const FfnArgs &a, void *stream);
 size_t gated_ffn_grad_workspace(const FfnArgs &a);
 int gated_ffn_grad(const FfnArgs &a, void *stream);
+// Tensors that the call's launches would not find apart, in words; empty: none.
+std::string gated_ffn_overlap(const FfnArgs &a);
+std::string gated_ffn_grad_overlap(const FfnArgs &a);
 // Text of a launcher's error; null from the host test library's launchers.
 const char *launch_error(int e);
 

@@ -334,6 +334,7 @@ Checks check_gated_ffn(const rtcc_gated_ffn_desc &d, rtcc::kern::FfnArgs &a) {
 Checks check_gated_ffn_forward(const rtcc_gated_ffn_desc &d, rtcc::kern::FfnArgs &a) {
     Checks c = check_gated_ffn(d, a);
     if (c.why.empty()) c.matrix(d.out, d.out_stride, d.rows, d.channels, a.bf16 ? 2 : 4, "out");
+    if (c.why.empty()) c.why = rtcc::kern::gated_ffn_overlap(a);
     return c;
 }
 
@@ -358,6 +359,7 @@ Checks check_gated_ffn_grad(const rtcc_gated_ffn_grad_desc &d, rtcc::kern::FfnAr
     a.dw_gate_s = d.dw_gate_stride;
     a.dw_up_s = d.dw_up_stride;
     a.dw_down_s = d.dw_down_stride;
+    if (c.why.empty()) c.why = rtcc::kern::gated_ffn_grad_overlap(a);
     return c;
 }
 

@@ -904,7 +904,8 @@ def gated_ffn_desc(x, w_gate, w_up, w_down, out, activation=RTCC_ACT_SILU, gate=
     """Description of a gated feed-forward unit: x, out [rows, channels]; w_gate,
     w_up [hidden, channels], w_down [channels, hidden]; gate, up, act [rows,
     hidden] of one stride, for the gradients, or None.  out may be None where
-    only the gradients are wanted."""
+    only the gradients are wanted, and may be x; otherwise no result may overlap
+    another tensor."""
     d = rtcc_gated_ffn_desc()
     if x.ndim != 2 or w_gate.ndim != 2:
         raise ValueError("x must be [rows, channels] and w_gate [hidden, channels]")
@@ -928,7 +929,8 @@ def gated_ffn_desc(x, w_gate, w_up, w_down, out, activation=RTCC_ACT_SILU, gate=
 
 def gated_ffn_grad_desc(fwd, dout, dx=None, dw_gate=None, dw_up=None, dw_down=None):
     """Description of the gradients of the call that fwd (gated_ffn_desc, with its
-    gate, up and act) describes; None: not wanted."""
+    gate, up and act) describes; None: not wanted.  No gradient may overlap another
+    tensor."""
     g = _grad_of(rtcc_gated_ffn_grad_desc, fwd)
     if _precision_of(dout) != fwd.precision:
         raise ValueError("dout must have the forward tensors' dtype")
