@@ -6,8 +6,11 @@
 //   dw = sum over rows of dy n,  db = sum over rows of dy
 //
 // G threads hold one row in registers, V times eight channels each (thread l:
-// channels 8 (l + G v) ..), so every tensor is read once and the variance is the
-// mean square of what is left without the mean.  Rows of up to 2,048 channels
+// channels 8 (l + G v) ..), so every tensor is read once.  The mean is taken twice: its
+// first sum is off by some 2^-20 of it, which is much beside the spread of a row far
+// from zero (n of a row of one value would be up to 1).  The differences from it are
+// exact there, and their sum, beside that of their squares, gives what is left of the
+// mean and the variance without it.  Rows of up to 2,048 channels
 // stay within a wave (G <= 64: sums by exchanges), longer ones take a block of
 // 256 or 512 threads (sums through LDS).  Bandwidth bound: 32,768 rows of 384
 // channels, bf16, with residual: 20.5 us, 4.9 TB/s, the rate of a copy; the gradient
@@ -117,6 +120,22 @@ __device__ inline void row_sums(float (&x)[N], float (*part)[2]) {
     }
 }
 
+// A row's first mean, rounded before it is taken from the row's values: the difference
+// of one with the unrounded product would itself be rounded.
+__device__ inline float first_mean(float sum, float over) {
+#pragma clang fp contract(off)
+    return sum * over;
+}
+// sum / channels, over = 1 / channels: exact where that is a float (equal differences),
+// in 3 instructions for a division's 10, which a row would wait for.
+__device__ inline float second_mean(float sum, float channels, float over) {
+    const float q = sum * over;
+    return fmaf(fmaf(-q, channels, sum), over, q);
+}
+// Sum of squares of a row's differences from its mean, from `left`, the sums of those
+// from the first mean and of their squares, and rest, the mean of the former.
+__device__ inline float square_sum(const float (&left)[2], float rest) { return fmaxf(fmaf(-rest, left[0], left[1]), 0.f); }
+
 template <int G>
 constexpr int kThreads = G > 256 ? G : 256;
 
@@ -131,7 +150,7 @@ __global__ __launch_bounds__(kThreads<G>) void k_layer_norm(LayerNormArgs a) {
     const float over = 1.f / float(a.channels);
     Eight<T> x[V], r[V];
     const T *px = static_cast<const T *>(a.x) + row * a.x_s, *pr = static_cast<const T *>(a.residual) + row * a.residual_s;
-    float s[V][8], sum[1] = {}, square[1] = {};
+    float s[V][8], sum[1] = {}, left[2] = {};
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int c = 8 * (l + G * v);
@@ -151,16 +170,18 @@ __global__ __launch_bounds__(kThreads<G>) void k_layer_norm(LayerNormArgs a) {
         if (on && a.sum_out) store8(static_cast<T *>(a.sum_out) + row * a.sum_s + 8 * (l + G * v), s[v]);
     }
     row_sums<G>(sum, part[0]);
-    const float mean = sum[0] / float(a.channels);
+    const float mean = first_mean(sum[0], over);
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             s[v][e] = 8 * (l + G * v) < a.channels ? s[v][e] - mean : 0.f;
-            square[0] = fmaf(s[v][e], s[v][e], square[0]);
+            left[0] += s[v][e];
+            left[1] = fmaf(s[v][e], s[v][e], left[1]);
         }
-    row_sums<G>(square, part[1]);
-    const float scale = rsqrtf(fmaf(square[0], over, a.eps));
+    row_sums<G>(left, part[1]);
+    const float rest = second_mean(left[0], float(a.channels), over);
+    const float scale = rsqrtf(fmaf(square_sum(left, rest), over, a.eps));
 #pragma unroll
     for (int v = 0; v < V; ++v) {
         const int c = 8 * (l + G * v);
@@ -170,7 +191,7 @@ __global__ __launch_bounds__(kThreads<G>) void k_layer_norm(LayerNormArgs a) {
         if (a.bias) load8_weight(a.bias + c, b);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            s[v][e] *= scale;
+            s[v][e] = (s[v][e] - rest) * scale;
             s[v][e] = fmaf(s[v][e], a.weight ? w[e] : 1.f, a.bias ? b[e] : 0.f);
         }
         store8(static_cast<T *>(a.out) + row * a.out_s + c, s[v]);
@@ -222,7 +243,7 @@ __global__ __launch_bounds__(kThreads<G>, 2) void k_layer_norm_grad(LayerNormArg
             fetch(row);
         }
         // channels past the end hold zeros
-        float n[V][8], y[V][8], past[V][8], sum[1] = {}, square[1] = {}, dots[2] = {};
+        float n[V][8], y[V][8], past[V][8], sum[1] = {}, left[2] = {}, dots[2] = {};
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
@@ -234,21 +255,23 @@ __global__ __launch_bounds__(kThreads<G>, 2) void k_layer_norm_grad(LayerNormArg
             }
         if (kAhead && row + ahead < a.rows) fetch(row + ahead);
         row_sums<G>(sum, part[0]);
-        const float mean = sum[0] / float(a.channels);
+        const float mean = first_mean(sum[0], over);
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 n[v][e] = 8 * (l + G * v) < a.channels ? n[v][e] - mean : 0.f;
-                square[0] = fmaf(n[v][e], n[v][e], square[0]);
+                left[0] += n[v][e];
+                left[1] = fmaf(n[v][e], n[v][e], left[1]);
             }
-        row_sums<G>(square, part[1]);
-        const float scale = rsqrtf(fmaf(square[0], over, a.eps));
+        row_sums<G>(left, part[1]);
+        const float rest = second_mean(left[0], float(a.channels), over);
+        const float scale = rsqrtf(fmaf(square_sum(left, rest), over, a.eps));
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                n[v][e] *= scale;
+                n[v][e] = (n[v][e] - rest) * scale;
                 dw[v][e] = fmaf(y[v][e], n[v][e], dw[v][e]);
                 db[v][e] += y[v][e];
                 y[v][e] *= w[v][e];
