@@ -11,8 +11,9 @@
 // from zero (n of a row of one value would be up to 1).  The differences from it are
 // exact there, and their sum, beside that of their squares, gives what is left of the
 // mean and the variance without it.  Rows of up to 2,048 channels
-// stay within a wave (G <= 64: sums by exchanges), longer ones take a block of
-// 256 or 512 threads (sums through LDS).  Bandwidth bound: 32,768 rows of 384
+// (of the gradient 1,536, of float32 with a gradient past the norm 1,024) stay within a
+// wave (G <= 64: sums by exchanges), longer ones take a block of 256 or 512 threads
+// (sums through LDS).  Bandwidth bound: 32,768 rows of 384
 // channels, bf16, with residual: 20.5 us, 4.9 TB/s, the rate of a copy; the gradient
 // with the one past the norm 21 us and 4 for the weights' sums (4.8 TB/s); float32
 // gradient of 4,577 rows of 4,104 channels 48 + 7 us.
@@ -356,7 +357,7 @@ __global__ __launch_bounds__(kSumChannels *kSumThreads) void k_layer_norm_sums(L
 struct Cut {
     int g, v;
 };
-Cut cut(int channels, int most) {
+constexpr Cut cut(int channels, int most) {
     const int eights = channels / 8;
     for (int g : {8, 16, 32, 64, 256, 512})
         if (eights <= most * g) return {g, (eights + g - 1) / g};
@@ -364,9 +365,18 @@ Cut cut(int channels, int most) {
 }
 // Three eights, of float32 with a gradient past the norm two: then the next row's fit
 // the registers beside this one's and the sums (2,281 rows of 7,712 channels, bf16, 512
-// threads with two: 40 us, 256 with four 86; 16,384 of 2,048: 56 us, 64 threads with
+// threads with two: 40 us, 256 with four 86; 16,384 of 2,048: 58 us, 64 threads with
 // four 99).
-Cut grad_cut(const LayerNormArgs &a) { return cut(a.channels, !a.bf16 && a.residual ? 2 : 3); }
+constexpr int grad_most(bool bf16, bool past) { return !bf16 && past ? 2 : 3; }
+Cut grad_cut(const LayerNormArgs &a) { return cut(a.channels, grad_most(a.bf16, a.residual)); }
+// Whether a row of some width is cut so: kernels of other cuts are not built.
+constexpr bool is_cut(int g, int v, int most) {
+    for (int channels = 8; channels <= kMaxNormChannels; channels += 8) {
+        const Cut c = cut(channels, most);
+        if (c.g == g && c.v == v) return true;
+    }
+    return false;
+}
 
 // Two blocks a CU, one of 512 threads: as many as fit it, and their sums stay small.
 int grad_blocks(const LayerNormArgs &a) {
@@ -376,14 +386,14 @@ int grad_blocks(const LayerNormArgs &a) {
 
 template <typename T, int G, int V>
 hipError_t run(const LayerNormArgs &a, int grad_blocks, hipStream_t s) {
-    if (grad_blocks) {
-        // of what grad_cut() gives
-        constexpr bool kPast = G == 512 || V <= (sizeof(T) == 4 ? 2 : 3), kAlone = G == 512 || V <= 3;
-        if constexpr (kPast)
-            if (a.residual) k_layer_norm_grad<T, G, V, true><<<grad_blocks, kThreads<G>, 0, s>>>(a);
-        if constexpr (kAlone)
-            if (!a.residual) k_layer_norm_grad<T, G, V, false><<<grad_blocks, kThreads<G>, 0, s>>>(a);
-    } else {
+    constexpr bool kBf16 = sizeof(T) == 2;
+    constexpr bool kForward = is_cut(G, V, 4), kPast = is_cut(G, V, grad_most(kBf16, true)),
+                   kAlone = is_cut(G, V, grad_most(kBf16, false));
+    if (grad_blocks && a.residual) {
+        if constexpr (kPast) k_layer_norm_grad<T, G, V, true><<<grad_blocks, kThreads<G>, 0, s>>>(a);
+    } else if (grad_blocks) {
+        if constexpr (kAlone) k_layer_norm_grad<T, G, V, false><<<grad_blocks, kThreads<G>, 0, s>>>(a);
+    } else if constexpr (kForward) {
         const Fold f = fold(row_tiles(a.rows, kThreads<G> / G), kThreads<G>);
         k_layer_norm<T, G, V><<<dim3(f.x, 1, f.z), kThreads<G>, 0, s>>>(a);
     }

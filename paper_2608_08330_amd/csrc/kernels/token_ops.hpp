@@ -103,6 +103,8 @@ constexpr int64_t kMaxRowStride = int64_t(1) << 22;
 // Of the gradient's smallest tiles of a long batch (64 keys): 2^29 + 2^26 blocks.
 constexpr int64_t kMaxGradKeys = int64_t(1) << 35;  // k_rows * kv_heads
 
+constexpr int32_t kMaxNormChannels = 16384;
+
 // rows * width of the feed-forward unit: its tiles, of 64 x 64 values at least,
 // are fewer than 2^29 with the rounded ones.
 constexpr int64_t kMaxFfnValues = int64_t(1) << 40;

@@ -20,7 +20,7 @@ constexpr int64_t kMaxRows = 2147483647;
 constexpr int64_t kMaxPlaces = 2147483648 - 256;
 constexpr int64_t kMaxRowStride = rtcc::kern::kMaxRowStride, kMaxHeadStride = int64_t(1) << 40;
 constexpr int32_t kMaxHeads = 1024, kMaxSeqs = 65536;
-constexpr int32_t kMaxNormChannels = 16384, kMaxFfnWidth = 65536;
+constexpr int32_t kMaxNormChannels = rtcc::kern::kMaxNormChannels, kMaxFfnWidth = 65536;
 
 // First failed check of a call; empty while all hold.
 struct Checks {
