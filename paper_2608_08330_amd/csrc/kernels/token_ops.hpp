@@ -105,8 +105,8 @@ constexpr int64_t kMaxGradKeys = int64_t(1) << 35;  // k_rows * kv_heads
 
 constexpr int32_t kMaxNormChannels = 16384;
 
-// rows * width of the feed-forward unit: its tiles, of 64 x 64 values at least,
-// are fewer than 2^29 with the rounded ones.
+// rows * width of the feed-forward unit: its tiles, of 64 x 32 values at least (of a
+// gated product, which has two of each), are fewer than 2^30 with the rounded ones.
 constexpr int64_t kMaxFfnValues = int64_t(1) << 40;
 
 size_t norm_rope_grad_workspace(const NormRopeArgs &a);

@@ -1,7 +1,8 @@
 // Prints the plans of the feed-forward unit's products on a device of 256 compute
-// units: for rows, channels, hidden (the arguments) and the strides of w_gate and
-// w_up, a line "product tile slices blocks" each.  Built and run by
-// tests/test_ffn_plans.py.
+// units: for bf16 or not, rows, channels, hidden and the strides of w_gate and w_up
+// (the arguments) a line "product tile slices blocks" each.  Without arguments: the
+// largest number of tiles that a product over the description's rows can have.  Built
+// and run by tests/test_ffn_plans.py.
 #include <cstdio>
 #include <cstdlib>
 
@@ -10,6 +11,15 @@
 using namespace rtcc::kern;
 
 int main(int argc, char **argv) {
+    if (argc == 1) {
+        int64_t most = 0;
+        for (int64_t n = 8; n <= 65536; n += 8)
+            for (Epilogue epi : {kPlain, kGated, kGatedGrad})
+                for (Tiles kind : {kTiles256, kTiles128, kTiles64, kTiles64Deep})
+                    most = std::max(most, tiles_of({std::min<int64_t>(2147483648 - 256, kMaxFfnValues / n), n}, kind, epi));
+        std::printf("%lld\n", (long long)most);
+        return 0;
+    }
     if (argc != 7) return 2;
     FfnArgs a{};
     a.bf16 = std::atoi(argv[1]);

@@ -14,14 +14,18 @@ UNITS = 256
 
 
 @pytest.fixture(scope="module")
-def plans(tmp_path_factory):
+def program(tmp_path_factory):
     exe = str(tmp_path_factory.mktemp("plans") / "ffn_plans")
     subprocess.run([B.CXX] + B.HOST_FLAGS + [os.path.join(NATIVE, "ffn_plans.cpp"), "-o", exe], check=True)
+    return exe
 
+
+@pytest.fixture
+def plans(program):
     def ask(rows, channels, hidden, strides=None, bf16=True):
         """product: (tile, slices, blocks)."""
         strides = strides or (channels, channels)
-        out = subprocess.run([exe] + [str(int(v)) for v in (bf16, rows, channels, hidden, *strides)], check=True,
+        out = subprocess.run([program] + [str(int(v)) for v in (bf16, rows, channels, hidden, *strides)], check=True,
                              stdout=subprocess.PIPE, text=True).stdout
         return {line.split()[0]: tuple(int(v) for v in line.split()[1:]) for line in out.splitlines()}
 
@@ -52,3 +56,9 @@ def test_strides_decide_the_tiles_of_dx(plans):
     for size in ((12400, 2056, 2056), (22801, 136, 3512), (121275, 136, 8), (16384, 2048, 8192)):
         p = plans(*size, (size[1] + 16, size[1] + 48))
         assert p.get("dx", p.get("dx_shared"))[0] < 256
+
+
+def test_most_tiles(program):
+    """Half tiles of 64 x 32 of a gated product, 2^40 / 520 rows of 520: more than 2^29."""
+    most = int(subprocess.run([program], check=True, stdout=subprocess.PIPE, text=True).stdout)
+    assert most == -(-(2 ** 40 // 520) // 64) * 17 == 561649570 < 1 << 30
