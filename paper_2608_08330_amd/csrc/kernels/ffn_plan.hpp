@@ -47,7 +47,10 @@ inline int64_t tiles_of(const Size &s, Tiles kind, Epilogue epi) {
 // 42 (46), 64 39; 32,768 x 384: 256 44 (46), 128 48 (50); three products of 1,536 x
 // 384, K 16,384: 256 in 7 slices 72 + 10 (80), 128 in 4 70 + 7 (84), 64 in 4 113 + 7;
 // 500 x 1,024, K 2,816: 64 with four buffers 12 (18), in 4 slices 11 + 5, 64 with two
-// 23 (26), 128 33 (35).
+// 23 (26), 128 33 (35).  It is low for the largest products (16,384 rows, 2,048
+// channels, 8,192 hidden: gate and up 982 us, 834 modelled, dX 842, 736, the weights
+// 1,208, 1,101) and for 256 with g and u stored over six steps (16,384 x 1,536: 62 to 73,
+// 51).
 struct Cost {
     int resident;                              // blocks of a CU
     double alone, shared;                      // a step of one block, and of each of several

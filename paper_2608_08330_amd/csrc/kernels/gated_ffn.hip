@@ -20,14 +20,14 @@
 // bf16 rounds what is stored and then multiplied: h, dG and dU (matrix operands), and
 // g and u where a gradient will read them.  Against 64-bit gradients dX, dWg and dWu
 // are 0.30% off (root mean square; rounding the result alone: 0.17%).  Stored in
-// float32, g and u would leave 0.24%, for 200 MB more traffic in the 270 us of a step
+// float32, g and u would leave 0.24%, for 200 MB more traffic in the 275 us of a step
 // over 16,384 rows of 384 channels, 1,536 hidden: some 40 us.  All sums are float32.
 //
 // What bounds them (kernel times of one MI355X): 16,384 rows, 2,048 channels, 8,192
-// hidden: matrix units 53 to 66% busy at 2.0 GHz (the power limit's clock), 1,100 to
-// 1,370 TFLOP/s; the LDS takes 2,560 cycles a step of 256 x 256 x 64 (64 KB written
+// hidden: matrix units 53 to 66% busy at 2.0 GHz (the power limit's clock), 1,120 to
+// 1,370 TFLOP/s (dG and dU 40%, 890: their tiles end in the most work); the LDS takes 2,560 cycles a step of 256 x 256 x 64 (64 KB written
 // at 64 bytes a cycle, 192 KB read at 128) beside 2,048 of products.  16,384 rows of
-// 384 channels, 1,536 hidden: 270 us a step with 1.0 GB of traffic (200 us at a copy's
+// 384 channels, 1,536 hidden: 275 us a step with 1.0 GB of traffic (200 us at a copy's
 // rate) and contracted axes of six steps, after which a tile's results cost as much.
 #include <algorithm>
 #include <initializer_list>
@@ -110,7 +110,7 @@ struct Work {
 // The product, the slice and the tile of a block.  Blocks of one XCD (every eighth)
 // take tiles that follow each other, in bands of kBand tiles of rows, so that their
 // operands meet in its L2.  A step over 16,384 rows of 2,048 channels, 8,192 hidden:
-// 3.90 ms in bands of 4, 3.92 of 2, 4.01 of 8, 4.07 of 16.
+// 4.05 ms in bands of 4, 4.07 of 2, 4.15 of 8, 4.20 of 16.
 struct Spot {
     int which, slice, tile_m, tile_n;  // which < 0: none, past the last one
 };
@@ -415,8 +415,8 @@ __global__ __launch_bounds__(256, 2) void k_products(Work x, Work w, uint32_t fi
 // first loads are under way while this one's results are stored.
 //
 // Four waves of 128 x 128 would read a third less from LDS; with the pipeline of
-// k_product (512 registers a lane) they took 4.2 ms for 3.9 in a step over 16,384 rows
-// of 2,048 channels, 8,192 hidden.  What is left is the end of a tile, which nothing
+// k_product (512 registers a lane) they took 8% longer in a step over 16,384 rows of
+// 2,048 channels, 8,192 hidden.  What is left is the end of a tile, which nothing
 // covers: 7 us of plain results, 12 with g and u stored, 27 of dG and dU (512 KB a
 // tile), beside 1.4 to 1.6 us a step.
 template <bool AK, bool BK, int EPI>
@@ -603,7 +603,8 @@ __global__ __launch_bounds__(512) void k_product_large(Work w) {
 // block has COLS (8 or 16) columns of the result; its eight waves share the
 // contracted axis in turns of 128 bytes, kTurns of them under way at a time, and
 // their sums are added up through LDS in the waves' order.  One row of 384 channels,
-// 1,536 hidden: 4 + 4 us, most of it the launch; as tiles 5 + 8.
+// 1,536 hidden: 4 + 4 us, most of it the launch; as tiles 5 + 8.  Of 4,096 channels,
+// 12,288 hidden: 59 us, 5.2 TB/s; 16 rows, whose x and h every block reads, 85.
 template <typename T, int EPI, int COLS>
 __global__ __launch_bounds__(512) void k_few(Work w) {
     constexpr int kMats = EPI == kGated ? 2 : 1, kTurns = 4, kWaves = 8, kPer = 16 / int(sizeof(T)), kTurn = 128 / int(sizeof(T));

@@ -13,10 +13,10 @@
 // mean and the variance without it.  Rows of up to 2,048 channels
 // (of the gradient 1,536, of float32 with a gradient past the norm 1,024) stay within a
 // wave (G <= 64: sums by exchanges), longer ones take a block of 256 or 512 threads
-// (sums through LDS).  Bandwidth bound: 32,768 rows of 384
-// channels, bf16, with residual: 20.5 us, 4.9 TB/s, the rate of a copy; the gradient
-// with the one past the norm 21 us and 4 for the weights' sums (4.8 TB/s); float32
-// gradient of 4,577 rows of 4,104 channels 48 + 7 us.
+// (sums through LDS).  Bandwidth bound: 32,768 rows of 384 channels, bf16, with
+// residual: 20.5 us, 4.9 TB/s, the rate of a copy; the gradient with the one past the
+// norm 22 us and 4 for the weights' sums (4.7 TB/s); float32 gradient of 4,577 rows of
+// 4,104 channels 47 + 7 us.
 #include <algorithm>
 
 #include <hip/hip_runtime.h>
@@ -201,7 +201,7 @@ __global__ __launch_bounds__(kThreads<G>) void k_layer_norm(LayerNormArgs a) {
 
 // A block walks rows and keeps the sums of its channels' dw and db in registers;
 // the next row's loads are under way while a row's sums are made (32,768 rows of 384:
-// 21 us; with sums by shuffles and each row's loads at its turn 34).  partial:
+// 22 us; with sums by shuffles and each row's loads at its turn 34).  partial:
 // [blocks][2][channels].  PAST: with dsum.
 template <typename T, int G, int V, bool PAST>
 __global__ __launch_bounds__(kThreads<G>, 2) void k_layer_norm_grad(LayerNormArgs a) {
