@@ -663,7 +663,7 @@ RTCC_API rtcc_status rtcc_attention_grad(const rtcc_attn_grad_desc *desc, void *
  * Tensors are [rows][channels] with an element stride between rows, channels
  * contiguous, rows 16-byte aligned; channels is a multiple of 8, at most 16384.
  * out and sum_out may each be x or residual, with the same stride, but not one
- * another. */
+ * another; any other overlap of theirs is refused (RTCC_E_ARG). */
 typedef struct rtcc_layer_norm_desc {
     int32_t abi_version;          /* RTCC_ABI_VERSION                                   */
     int32_t precision;            /* rtcc_precision of x, residual, sum_out, out        */
@@ -682,11 +682,12 @@ RTCC_API rtcc_status rtcc_layer_norm(const rtcc_layer_norm_desc *desc, void *hip
  * and required then; else x) and weight are read.  dout: the gradient of out;
  * dsum, if given, the gradient that reaches the sum past the norm.  dx: the
  * gradient of x, and of residual alike, dsum added; it may be dout or dsum or
- * the normed tensor, with the same stride.  dweight, dbias: float32 [channels],
- * written, not added to; summed over the rows in a fixed order; NULL: not
- * wanted.  workspace: device memory of at least rtcc_layer_norm_grad_workspace
- * bytes, 16-byte aligned (NULL where that is 0); it needs no initial contents, and
- * calls that may run at once need one each. */
+ * the normed tensor, with the same stride; any other overlap with them is
+ * refused (RTCC_E_ARG), as is one of dweight with dbias.  dweight, dbias:
+ * float32 [channels], written, not added to; summed over the rows in a fixed
+ * order; NULL: not wanted.  workspace: device memory of at least
+ * rtcc_layer_norm_grad_workspace bytes, 16-byte aligned (NULL where that is 0);
+ * it needs no initial contents, and calls that may run at once need one each. */
 typedef struct rtcc_layer_norm_grad_desc {
     rtcc_layer_norm_desc fwd;
     const void *dout, *dsum;

@@ -7,6 +7,7 @@
 #include <string>
 
 #include "../../include/rtcc.h"
+#include "kernels/matrix_overlap.hpp"
 #include "kernels/token_ops.hpp"
 
 namespace rtcc {
@@ -242,6 +243,17 @@ Checks check_attention_grad(const rtcc_attn_grad_desc &d, rtcc::kern::AttnArgs &
 
 int64_t row_stride(int64_t stride, int64_t rows, int32_t width) { return rows > 1 ? stride : width; }
 
+// Of a layer norm: a result may take a tensor's place row by row, that is with its
+// stride; another row that is still to be read must not be under it.
+void in_place_or_apart(Checks &c, const rtcc::kern::LayerNormArgs &a, const void *out, int64_t out_stride, const char *name,
+                       const void *in, int64_t in_stride, const char *other) {
+    if (!c.why.empty() || (out == in && out_stride == in_stride)) return;
+    const int32_t elem = a.bf16 ? 2 : 4;
+    if (overlap(rtcc::kern::extent(out, a.rows, out_stride, a.channels, elem),
+                rtcc::kern::extent(in, a.rows, in_stride, a.channels, elem)))
+        c.why = std::string(name) + " overlaps " + other + " and is not in its place";
+}
+
 // The part of a layer norm's call that forward and gradient share.
 Checks check_layer_norm(const rtcc_layer_norm_desc &d, rtcc::kern::LayerNormArgs &a) {
     Checks c;
@@ -281,6 +293,12 @@ Checks check_layer_norm_grad(const rtcc_layer_norm_grad_desc &d, rtcc::kern::Lay
     a.out_s = row_stride(d.dx_stride, f.rows, f.channels);
     a.dweight = d.dweight;
     a.dbias = d.dbias;
+    in_place_or_apart(c, a, a.out, a.out_s, "dx", a.x, a.x_s, f.residual ? "sum_out" : "x");
+    in_place_or_apart(c, a, a.out, a.out_s, "dx", a.dout, a.dout_s, "dout");
+    if (d.dsum) in_place_or_apart(c, a, a.out, a.out_s, "dx", a.residual, a.residual_s, "dsum");
+    const int64_t each = a.channels;
+    c.need(!overlap(rtcc::kern::extent(d.dweight, 1, each, each, 4), rtcc::kern::extent(d.dbias, 1, each, each, 4)),
+           "dweight overlaps dbias");
     return c;
 }
 
@@ -507,6 +525,13 @@ rtcc_status rtcc_layer_norm(const rtcc_layer_norm_desc *desc, void *hip_stream) 
             a.residual_s = row_stride(d.residual_stride, d.rows, d.channels);
             a.sum_s = row_stride(d.sum_out_stride, d.rows, d.channels);
             a.out_s = row_stride(d.out_stride, d.rows, d.channels);
+            in_place_or_apart(c, a, a.out, a.out_s, "out", a.x, a.x_s, "x");
+            if (a.residual) in_place_or_apart(c, a, a.out, a.out_s, "out", a.residual, a.residual_s, "residual");
+            if (a.sum_out) {
+                in_place_or_apart(c, a, a.sum_out, a.sum_s, "sum_out", a.x, a.x_s, "x");
+                if (a.residual) in_place_or_apart(c, a, a.sum_out, a.sum_s, "sum_out", a.residual, a.residual_s, "residual");
+                in_place_or_apart(c, a, a.sum_out, a.sum_s, "sum_out", a.out, a.out_s, "out");
+            }
         }
         if (!c.why.empty()) return fail(RTCC_E_ARG, c.why);
         if (d.rows == 0) return RTCC_OK;
